@@ -385,6 +385,107 @@ XRED_API xred_status xred_allreduce_sim(const void *const *sendbufs, void *const
 XRED_API size_t xred_sim_chunk(size_t count, int nranks);
 
 /*
+ * ------------------------------------------------ around a reduced activation --
+ * The calls below take what a reduction over ranks produced on to the next
+ * one: the partial sums of a tensor-parallel layer are folded, joined with the
+ * residual stream and normalised in one pass (xred_fold_norm); a mixture of
+ * experts then picks each token's experts (xred_route), orders the rows by
+ * expert -- counts and offsets are the metadata of the AllToAllv that carries
+ * them, resident on the GPU as in Section 6.1 -- (xred_dispatch_plan,
+ * xred_dispatch) and reduces the experts' rows back to tokens (xred_combine).
+ * The *_grad calls are their backward passes.
+ *
+ * Shared conventions, besides those at the top of this file:
+ *   - dtype is XRED_FLOAT32, XRED_BFLOAT16 or XRED_FLOAT16 unless stated;
+ *     all arithmetic, sums and statistics are binary32, and each output is
+ *     rounded once, as down() above rounds.
+ *   - Matrices are row-major with a distance between rows (xred_rows); rows
+ *     need only be aligned to their element.
+ *   - Nothing is allocated and nothing is kept between calls, so every call
+ *     can be captured in a HIP graph; calls that need scratch memory take it
+ *     from the caller (workspace, at least the size the *_workspace function
+ *     gives, 16-byte aligned; its contents need not be kept or cleared).
+ *   - Results do not depend on the CU budget or on the order in which
+ *     workgroups run (no floating-point atomics).
+ *   - An output may not overlap any other buffer of the call unless stated.
+ *   - Errors: XRED_INVALID_ARGUMENT, XRED_UNSUPPORTED (types and sizes),
+ *     XRED_ALIAS, XRED_HIP_ERROR; zero rows or tokens succeed with no launch
+ *     where nothing is to be written.
+ */
+
+/* Row r of a matrix starts r * stride elements after data; stride is at least
+ * the row's length.  data NULL: the matrix is absent. */
+typedef struct {
+    void *data;
+    uint64_t stride;
+} xred_rows;
+
+enum { XRED_MAX_HIDDEN = 32768 };  /* elements of a row xred_fold_norm keeps on chip */
+enum { XRED_MAX_EXPERTS = 1024, XRED_MAX_TOPK = 32, XRED_MAX_EXPERT_GROUPS = 64 };
+
+/*
+ * Fold of P partial sums, residual addition and root-mean-square norm:
+ *     h      = (up(src[0]) + up(src[1]) + ... + up(src[P-1])) + up(residual)
+ *     rstd   = 1 / sqrt(mean(h^2) + eps)                  (one value a row)
+ *     y      = h * (rstd * up(weight))
+ *     sum    = down(h),  out = down(y)
+ *     out8   = e4m3(y / scale),  scale = max(amax, 2^-100) / 448, amax the
+ *              largest |y| of the group (a NaN in a group gives NaN)
+ * h is not rounded before it is normalised.
+ *   srcs      host array of nsrc (1..XRED_MAX_SRC) device pointers, rows x
+ *             hidden each, all with row distance src_stride; read before return
+ *   residual  optional; weight: hidden elements of weight_dtype (dtype or
+ *             XRED_FLOAT32), NULL: ones
+ *   sum, out, out8, rstd   outputs, each optional, at least one of out and
+ *             out8 present.  sum and out may each be one of the inputs (the
+ *             same pointer and stride), out only where sum is another.
+ *   scale     rows x ceil(hidden / group) binary32, present with out8
+ *   group     elements of a row that share a scale: 32, 64, 128, 256 or 512
+ *             (the last group may be short), or 0 for the whole row
+ *   hidden    1..XRED_MAX_HIDDEN (else XRED_UNSUPPORTED)
+ */
+typedef struct {
+    const void *const *srcs;
+    uint64_t src_stride;
+    uint32_t nsrc;
+    uint32_t group;
+    uint64_t rows, hidden;
+    xred_rows residual, sum, out, out8, scale;
+    const void *weight;
+    float *rstd;
+    xred_dtype dtype, weight_dtype;
+    float eps;
+} xred_fold_norm_args;
+XRED_API xred_status xred_fold_norm(const xred_fold_norm_args *args, void *hip_stream);
+
+/*
+ * The gradient of xred_fold_norm's out:
+ *     g       = up(dout) * up(weight),  n = up(sum) * rstd
+ *     dx      = down(rstd * (g - n * mean(g * n)) + up(dsum))
+ *     dweight = sum over rows of up(dout) * n             (binary32)
+ * dx is the gradient of the residual and of every source alike.
+ *   sum, rstd  what xred_fold_norm wrote;  dsum: optional, the gradient that
+ *              reaches `sum` itself along the residual stream
+ *   dx         may be dout or dsum (the same pointer and stride)
+ *   dweight    hidden binary32 values, optional; set (to zero where there are
+ *              no rows), not added to.  It needs the workspace.
+ */
+typedef struct {
+    uint64_t rows, hidden;
+    xred_rows dout, sum, dsum, dx;
+    const void *weight;
+    const float *rstd;
+    float *dweight;
+    void *workspace;
+    uint64_t workspace_bytes;
+    xred_dtype dtype, weight_dtype;
+} xred_fold_norm_grad_args;
+XRED_API xred_status xred_fold_norm_grad(const xred_fold_norm_grad_args *args, void *hip_stream);
+
+/* Bytes of workspace xred_fold_norm_grad needs for dweight. */
+XRED_API size_t xred_fold_norm_grad_workspace(uint64_t rows, uint64_t hidden);
+
+/*
  * CU budget: at most max_workgroups workgroups per launch of the fused,
  * reduce-scatter, step-wise, cast and batched kernels (0 = no limit, the
  * default), so a reduction can run beside compute kernels on the rest of the

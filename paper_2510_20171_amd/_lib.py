@@ -41,10 +41,32 @@ class XredItem(ctypes.Structure):
                 ("nsrc", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
+class XredRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_uint64)]
+
+
+def _struct(name, fields):
+    """A ctypes structure from "type name" lines: p pointer, r rows, q/u 64/32-bit, i enum, f float."""
+    types = {"p": ctypes.c_void_p, "r": XredRows, "q": ctypes.c_uint64, "u": ctypes.c_uint32,
+             "i": ctypes.c_int, "f": ctypes.c_float}
+    pairs = [(n, types[t]) for t, *names in map(str.split, fields) for n in names]
+    return type(name, (ctypes.Structure,), {"_fields_": pairs})
+
+
+# The argument structures of include/xred.h, field for field.
+FoldNormArgs = _struct("FoldNormArgs", [
+    "p srcs", "q src_stride", "u nsrc group", "q rows hidden",
+    "r residual sum out out8 scale", "p weight rstd", "i dtype weight_dtype", "f eps"])
+FoldNormGradArgs = _struct("FoldNormGradArgs", [
+    "q rows hidden", "r dout sum dsum dx", "p weight rstd dweight workspace",
+    "q workspace_bytes", "i dtype weight_dtype"])
+
 EXPORTS = ("xred_allreduce_local", "xred_reduce_scatter_local", "xred_reduce_copy_step",
            "xred_acc_cast", "xred_batched_reduce", "xred_batched_reduce_noalloc",
            "xred_ring_reduce", "xred_ring_max_count",
-           "xred_allreduce_sim", "xred_sim_chunk", "xred_set_max_workgroups",
+           "xred_allreduce_sim", "xred_sim_chunk",
+           "xred_fold_norm", "xred_fold_norm_grad", "xred_fold_norm_grad_workspace",
+           "xred_set_max_workgroups",
            "xred_stream_create_partition", "xred_stream_destroy", "xred_acc_elem_size",
            "xred_status_string",
            "xred_last_error", "xred_version", "xred_release")
@@ -98,6 +120,11 @@ def load(path: Path = LIB_PATH) -> ctypes.CDLL:
         getattr(L, f).restype = ctypes.c_int
     L.xred_stream_create_partition.argtypes = [i32, ctypes.POINTER(vp), ctypes.POINTER(vp)]
     L.xred_stream_destroy.argtypes = [vp]
+    for f in ("xred_fold_norm", "xred_fold_norm_grad"):
+        getattr(L, f).argtypes = [vp, vp]
+        getattr(L, f).restype = ctypes.c_int
+    L.xred_fold_norm_grad_workspace.argtypes = [ctypes.c_uint64, ctypes.c_uint64]
+    L.xred_fold_norm_grad_workspace.restype = sz
     L.xred_set_max_workgroups.argtypes = [ctypes.c_uint]
     L.xred_set_max_workgroups.restype = ctypes.c_uint
     L.xred_acc_elem_size.argtypes = [i32]

@@ -52,10 +52,8 @@ void trace_launch(const void *kernel, dim3 grid, dim3 block, size_t lds, hipStre
     free(name);
 }
 
-namespace {
-
 constexpr int kMaxDevices = 64;
-thread_local char g_err[512];
+static thread_local char g_err[512];
 
 xred_status fail(xred_status s, const char *fmt, ...)
 {
@@ -71,6 +69,8 @@ xred_status hip_fail(hipError_t e, const char *what)
 {
     return fail(XRED_HIP_ERROR, "%s: %s", what, hipGetErrorString(e));
 }
+
+namespace {
 
 bool known_dtype(xred_dtype d) { return d >= XRED_FLOAT32 && d <= XRED_UINT8; }
 bool known_op(xred_op o) { return o >= XRED_SUM && o <= XRED_AVG; }
@@ -102,6 +102,8 @@ xred_status check_types(xred_dtype dtype, xred_op op)
     return XRED_SUCCESS;
 }
 
+}  // namespace
+
 // A buffer of `bytes` at p: non-NULL, aligned to `align`, no address wrap.
 // align: a power of two (an element or accumulator size)
 xred_status check_buf(const void *p, size_t bytes, size_t align, const char *name, int index)
@@ -129,6 +131,8 @@ bool mul_overflows(size_t a, size_t b)
     size_t r;
     return __builtin_mul_overflow(a, b, &r);
 }
+
+namespace {
 
 int cached_cus[kMaxDevices];
 int cached_lds[kMaxDevices];

@@ -49,6 +49,18 @@ hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds
                               std::index_sequence_for<P...>{}, std::forward<A>(args)...);
 }
 
+// Records the calling thread's error text (xred_last_error) and returns s.
+xred_status fail(xred_status s, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+xred_status hip_fail(hipError_t e, const char *what);
+
+// A buffer of `bytes` at p: non-NULL, aligned to `align` (a power of two), no
+// address wrap.
+xred_status check_buf(const void *p, size_t bytes, size_t align, const char *name, int index);
+// Overlap of [a, a+na) and [b, b+nb), other than the identical range when
+// `exact_ok`.
+bool bad_overlap(const void *a, size_t na, const void *b, size_t nb, bool exact_ok);
+bool mul_overflows(size_t a, size_t b);
+
 // Workgroup budget for one launch on the current device: the number of tiles,
 // capped by XRED_MAX_WORKGROUPS when set (a CU-budget knob: it never changes
 // results, only how many workgroups share the work).

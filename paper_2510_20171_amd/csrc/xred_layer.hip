@@ -1,0 +1,185 @@
+// xred_layer.hip -- the C ABI of the calls around a reduced activation:
+// argument checks and dispatch to the launchers (xred_norm.hip).  As
+// elsewhere, everything is checked before anything is enqueued.
+#include "xred_layer.hpp"
+
+namespace xred {
+namespace {
+
+bool row_type(xred_dtype d)
+{
+    return d == XRED_FLOAT32 || d == XRED_BFLOAT16 || d == XRED_FLOAT16;
+}
+
+// A matrix of the call: where its rows lie, in bytes.
+struct Matrix {
+    const void *data;
+    uint64_t stride, width, rows;   // bytes between rows, bytes of a row
+    uint64_t span() const { return (rows - 1) * stride + width; }
+};
+
+// m (present, at least one row of at least one element) as a Matrix.
+xred_status check_rows(const xred_rows &m, uint64_t rows, uint64_t columns, uint64_t es,
+                       const char *name, Matrix *out)
+{
+    if (m.stride < columns)
+        return fail(XRED_INVALID_ARGUMENT, "%s: row distance %llu is below the row's %llu elements",
+                    name, (unsigned long long)m.stride, (unsigned long long)columns);
+    uint64_t bytes;
+    if (__builtin_mul_overflow(m.stride, es, &bytes) || mul_overflows(bytes, rows))
+        return fail(XRED_INVALID_ARGUMENT, "%s: size overflows", name);
+    *out = Matrix{m.data, bytes, columns * es, rows};
+    return check_buf(m.data, out->span(), es, name, 0);
+}
+
+// Whether rows of a and b share a byte, other than being the same rows when
+// `exact_ok`.  Matrices at one row distance may interleave (column ranges of
+// one larger matrix); at different distances their whole spans count.
+bool rows_overlap(const Matrix &a, const Matrix &b, bool exact_ok)
+{
+    if (a.data == b.data && a.stride == b.stride && a.width == b.width && exact_ok) return false;
+    if (!bad_overlap(a.data, a.span(), b.data, b.span(), false)) return false;
+    if (a.stride != b.stride) return true;
+    const uintptr_t x = (uintptr_t)a.data, y = (uintptr_t)b.data;
+    const uint64_t s = a.stride, d = y >= x ? (y - x) % s : (s - (x - y) % s) % s;
+    return d < a.width || s - d < b.width;
+}
+
+xred_status check_weight(const void *w, xred_dtype wt, xred_dtype dtype, uint64_t hidden,
+                         Matrix *out)
+{
+    if (wt != dtype && wt != XRED_FLOAT32)
+        return fail(XRED_UNSUPPORTED, "weight_dtype %d with dtype %d", (int)wt, (int)dtype);
+    return check_rows(xred_rows{(void *)w, hidden}, 1, hidden, elem_size(wt), "weight", out);
+}
+
+// No output shares bytes with another matrix of the call.  may[i]: the output
+// out[i] may be exactly one of the first n[i] inputs.
+xred_status check_apart(const Matrix *out, const char *const *names, int nout, const Matrix *in,
+                        int nin, const int *may)
+{
+    for (int i = 0; i < nout; ++i) {
+        for (int j = 0; j < nin; ++j)
+            if (rows_overlap(out[i], in[j], j < may[i]))
+                return fail(XRED_ALIAS, "%s overlaps an input", names[i]);
+        for (int j = 0; j < i; ++j)
+            if (rows_overlap(out[i], out[j], false))
+                return fail(XRED_ALIAS, "%s overlaps %s", names[i], names[j]);
+    }
+    return XRED_SUCCESS;
+}
+
+}  // namespace
+}  // namespace xred
+
+using namespace xred;
+
+#define TRY(call)                                    \
+    do {                                             \
+        const xred_status st_ = (call);              \
+        if (st_ != XRED_SUCCESS) return st_;         \
+    } while (0)
+
+extern "C" {
+
+XRED_API xred_status xred_fold_norm(const xred_fold_norm_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_fold_norm_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_fold_norm nsrc=%u rows=%llu hidden=%llu dtype=%d group=%u stream=%p",
+                     a.nsrc, (unsigned long long)a.rows, (unsigned long long)a.hidden,
+                     (int)a.dtype, a.group, hip_stream);
+    if (a.nsrc < 1 || a.nsrc > XRED_MAX_SRC)
+        return fail(XRED_INVALID_ARGUMENT, "nsrc = %u outside 1..%d", a.nsrc, XRED_MAX_SRC);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    if (a.hidden < 1 || a.hidden > XRED_MAX_HIDDEN)
+        return fail(XRED_UNSUPPORTED, "hidden = %llu outside 1..%d", (unsigned long long)a.hidden,
+                    XRED_MAX_HIDDEN);
+    if (!(a.eps >= 0.0f)) return fail(XRED_INVALID_ARGUMENT, "eps is negative or a NaN");
+    if (a.group != 0 && (a.group < 32 || a.group > 512 || (a.group & (a.group - 1))))
+        return fail(XRED_INVALID_ARGUMENT, "group = %u is not 0, 32, 64, 128, 256 or 512", a.group);
+    if (a.rows == 0) return XRED_SUCCESS;   // buffers of no rows may be NULL
+    if (!a.out.data && !a.out8.data)
+        return fail(XRED_INVALID_ARGUMENT, "neither out nor out8 is given");
+    if ((a.out8.data == nullptr) != (a.scale.data == nullptr))
+        return fail(XRED_INVALID_ARGUMENT, "out8 and scale go together");
+    if (a.srcs == nullptr) return fail(XRED_INVALID_ARGUMENT, "srcs is NULL");
+    const uint64_t es = elem_size(a.dtype);
+    Matrix in[XRED_MAX_SRC + 2], out[5];
+    const char *names[5];
+    int nin = 0, nout = 0, may[5];
+    for (uint32_t p = 0; p < a.nsrc; ++p)
+        TRY(check_rows(xred_rows{(void *)a.srcs[p], a.src_stride}, a.rows, a.hidden, es, "srcs",
+                       &in[nin++]));
+    if (a.residual.data)
+        TRY(check_rows(a.residual, a.rows, a.hidden, es, "residual", &in[nin++]));
+    const int same = nin;
+    if (a.weight) TRY(check_weight(a.weight, a.weight_dtype, a.dtype, a.hidden, &in[nin++]));
+    auto output = [&](const xred_rows &m, uint64_t columns, uint64_t size, const char *name,
+                      int in_place) {
+        names[nout] = name;
+        may[nout] = in_place;
+        return m.data ? check_rows(m, a.rows, columns, size, name, &out[nout++]) : XRED_SUCCESS;
+    };
+    TRY(output(a.sum, a.hidden, es, "sum", same));
+    TRY(output(a.out, a.hidden, es, "out", same));
+    TRY(output(a.out8, a.hidden, 1, "out8", 0));
+    TRY(output(a.scale, a.group ? (a.hidden + a.group - 1) / a.group : 1, 4, "scale", 0));
+    TRY(output(xred_rows{a.rstd, 1}, 1, 4, "rstd", 0));
+    TRY(check_apart(out, names, nout, in, nin, may));
+    const hipError_t e = launch_fold_norm(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "fold_norm launch");
+}
+
+XRED_API size_t xred_fold_norm_grad_workspace(uint64_t rows, uint64_t hidden)
+{
+    return hidden > XRED_MAX_HIDDEN ? 0 : (size_t)norm_grad_slices(rows) * hidden * 4;
+}
+
+XRED_API xred_status xred_fold_norm_grad(const xred_fold_norm_grad_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_fold_norm_grad_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_fold_norm_grad rows=%llu hidden=%llu dtype=%d stream=%p",
+                     (unsigned long long)a.rows, (unsigned long long)a.hidden, (int)a.dtype,
+                     hip_stream);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    if (a.hidden < 1 || a.hidden > XRED_MAX_HIDDEN)
+        return fail(XRED_UNSUPPORTED, "hidden = %llu outside 1..%d", (unsigned long long)a.hidden,
+                    XRED_MAX_HIDDEN);
+    if (a.rows == 0 && !a.dweight) return XRED_SUCCESS;
+    const uint64_t es = elem_size(a.dtype);
+    Matrix in[5], out[3];
+    const char *names[3];
+    int nin = 0, nout = 0, may[3] = {0, 0, 0};
+    if (a.rows) {
+        TRY(check_rows(a.dout, a.rows, a.hidden, es, "dout", &in[nin++]));
+        if (a.dsum.data) TRY(check_rows(a.dsum, a.rows, a.hidden, es, "dsum", &in[nin++]));
+        may[0] = nin;
+        TRY(check_rows(a.sum, a.rows, a.hidden, es, "sum", &in[nin++]));
+        TRY(check_rows(xred_rows{(void *)a.rstd, 1}, a.rows, 1, 4, "rstd", &in[nin++]));
+        if (a.weight) TRY(check_weight(a.weight, a.weight_dtype, a.dtype, a.hidden, &in[nin++]));
+        names[nout] = "dx";
+        TRY(check_rows(a.dx, a.rows, a.hidden, es, "dx", &out[nout++]));
+    }
+    if (a.dweight) {
+        names[nout] = "dweight";
+        TRY(check_rows(xred_rows{a.dweight, a.hidden}, 1, a.hidden, 4, "dweight", &out[nout++]));
+        const uint64_t need = xred_fold_norm_grad_workspace(a.rows, a.hidden);
+        if (a.workspace_bytes < need)
+            return fail(XRED_INVALID_ARGUMENT, "workspace of %llu bytes, %llu are needed",
+                        (unsigned long long)a.workspace_bytes, (unsigned long long)need);
+        if (need) {
+            TRY(check_buf(a.workspace, need, 16, "workspace", 0));
+            names[nout] = "workspace";
+            out[nout++] = Matrix{a.workspace, need, need, 1};
+        }
+    }
+    TRY(check_apart(out, names, nout, in, nin, may));
+    const hipError_t e = launch_fold_norm_grad(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "fold_norm_grad launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,16 @@
+// xred_layer.hpp -- launchers behind the calls around a reduced activation
+// (norm, routing, dispatch, combine).  Arguments were validated by the caller
+// (xred_layer.hip).
+#pragma once
+
+#include "xred_dispatch.hpp"
+#include "xred_internal.hpp"
+
+namespace xred {
+
+hipError_t launch_fold_norm(const xred_fold_norm_args &a, hipStream_t stream);
+// Rows of the gradient's partial sums of dweight.
+uint32_t norm_grad_slices(uint64_t rows);
+hipError_t launch_fold_norm_grad(const xred_fold_norm_grad_args &a, hipStream_t stream);
+
+}  // namespace xred

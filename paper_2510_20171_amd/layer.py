@@ -1,0 +1,143 @@
+"""The calls around a reduced activation: fold of partial sums with residual
+addition and norm, expert routing, dispatch and combine, with their gradients
+(the second half of include/xred.h).
+
+Matrices are 2-D GPU tensors whose rows are contiguous; rows may lie further
+apart than their length (a column range of a larger matrix).  Outputs are the
+caller's tensors, written in place on the current stream (or ``stream``).
+
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    xr.fold_norm(partial_sums, y, residual=x, weight=w, sum=h)   # h = x + sum, y = norm(h)
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import _dtype_name, _ptr, _require, _stream
+from ._lib import (DTYPE, ELEM_SIZE, INVALID_ARGUMENT, FoldNormArgs, FoldNormGradArgs, XredError,
+                   XredRows, check, load, ptr_array)
+
+
+def _refuse(text):
+    raise XredError(INVALID_ARGUMENT, text)
+
+
+def _matrix(t, rows, columns, es, what, device):
+    """t as an xred_rows after checking its shape, element size and device; None: absent."""
+    if t is None:
+        return XredRows(None, 0)
+    if not t.is_cuda or t.device != device:
+        _refuse(f"{what} is on {t.device}, not {device}")
+    if tuple(t.shape) != (rows, columns):
+        _refuse(f"{what} has shape {tuple(t.shape)}, expected {(rows, columns)}")
+    if t.element_size() != es:
+        _refuse(f"{what} has {t.element_size()}-byte elements, expected {es}")
+    if columns > 1 and t.stride(1) != 1:
+        _refuse(f"{what}: elements of a row are not contiguous")
+    # the distance of one row from the next means nothing for a single row
+    return XredRows(t.data_ptr(), t.stride(0) if rows > 1 else columns)
+
+
+def _shape(t, what):
+    if t.dim() != 2:
+        _refuse(f"{what} has {t.dim()} dimensions, expected 2")
+    if not t.is_cuda:
+        _refuse(f"{what} is not in GPU memory")
+    return t.shape[0], t.shape[1]
+
+
+def _vector(t, n, es, what, device):
+    _require([t], n, es, what, device)
+    return _ptr(t)
+
+
+def _floats(t, n, what, device):
+    if t is not None and _dtype_name(t, None) != "f32":
+        _refuse(f"{what} is {t.dtype}, expected float32")
+    return _vector(t, n, 4, what, device)
+
+
+def _weight(t, dtype, n, device):
+    """(pointer, dtype code) of a row of weights in dtype or fp32; None: ones."""
+    name = dtype if t is None else _dtype_name(t, None)
+    if name not in (dtype, "f32"):
+        _refuse(f"weight is {name}, expected {dtype} or f32")
+    return _vector(t, n, ELEM_SIZE[name], "weight", device), DTYPE[name]
+
+
+def _workspace(t, nbytes, like, stream):
+    """The caller's workspace, or one from torch's allocator."""
+    import torch
+    if t is None:
+        t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+        if stream is not None:   # else it belongs to the stream the call runs on
+            if not isinstance(stream, torch.cuda.Stream):
+                handle = int(getattr(stream, "cuda_stream", stream))
+                stream = torch.cuda.ExternalStream(handle, device=like.device)
+            t.record_stream(stream)
+    elif not t.is_cuda or t.device != like.device or not t.is_contiguous():
+        _refuse("workspace is not a contiguous tensor of the call's device")
+    return t
+
+
+def fold_norm(srcs, out=None, *, residual=None, weight=None, sum=None, out8=None, scale=None,
+              rstd=None, group: int = 0, eps: float = 1e-6, stream=None) -> None:
+    """Fold of partial sums, residual addition and RMS norm (xred_fold_norm).
+
+    h = srcs[0] + ... + srcs[P-1] + residual; sum = h, out = h * rstd * weight,
+    out8 the same in e4m3 with a scale for each row (group = 0) or group of
+    elements; rstd the rows' 1 / sqrt(mean(h^2) + eps).  All but one of out and
+    out8 is optional."""
+    if len(srcs) < 1:
+        _refuse("no sources")
+    rows, hidden = _shape(srcs[0], "srcs[0]")
+    dt, dev = _dtype_name(srcs[0], None), srcs[0].device
+    es = ELEM_SIZE[dt]
+    src = [_matrix(s, rows, hidden, es, f"srcs[{k}]", dev) for k, s in enumerate(srcs)]
+    if any(m.stride != src[0].stride for m in src):
+        _refuse("srcs have different row distances")
+    for what, t in (("residual", residual), ("sum", sum), ("out", out), *(
+            (f"srcs[{k}]", s) for k, s in enumerate(srcs))):
+        if t is not None and t.dtype != srcs[0].dtype:
+            _refuse(f"{what} is {t.dtype}, srcs[0] is {srcs[0].dtype}")
+    if out8 is not None and _dtype_name(out8, None) not in ("e4m3", "u8"):
+        _refuse(f"out8 is {out8.dtype}, expected float8_e4m3fn or uint8")
+    if scale is not None and _dtype_name(scale, None) != "f32":
+        _refuse(f"scale is {scale.dtype}, expected float32")
+    groups = -(-hidden // group) if group > 0 else 1
+    w, wt = _weight(weight, dt, hidden, dev)
+    ptrs = ptr_array([m.data or 0 for m in src])
+    a = FoldNormArgs(
+        ctypes.addressof(ptrs), src[0].stride, len(src), group, rows, hidden,
+        _matrix(residual, rows, hidden, es, "residual", dev),
+        _matrix(sum, rows, hidden, es, "sum", dev), _matrix(out, rows, hidden, es, "out", dev),
+        _matrix(out8, rows, hidden, 1, "out8", dev),
+        _matrix(scale, rows, groups, 4, "scale", dev), w, _floats(rstd, rows, "rstd", dev),
+        DTYPE[dt], wt, eps)
+    check(load().xred_fold_norm(ctypes.byref(a), _stream(srcs[0], stream)))
+
+
+def fold_norm_grad(dout, sum, rstd, dx, *, weight=None, dsum=None, dweight=None, workspace=None,
+                   stream=None) -> None:
+    """The gradient of fold_norm's out (xred_fold_norm_grad): dx, the gradient of
+    the residual and of every source, and dweight (fp32).  dsum: the gradient
+    that reaches fold_norm's sum; workspace: a tensor to use for dweight's
+    partial sums instead of one from torch's allocator."""
+    rows, hidden = _shape(sum, "sum")
+    dt, dev = _dtype_name(sum, None), sum.device
+    es = ELEM_SIZE[dt]
+    for what, t in (("dout", dout), ("dsum", dsum), ("dx", dx)):
+        if t is not None and t.dtype != sum.dtype:
+            _refuse(f"{what} is {t.dtype}, sum is {sum.dtype}")
+    L = load()
+    ws = None
+    if dweight is not None:
+        ws = _workspace(workspace, L.xred_fold_norm_grad_workspace(rows, hidden), sum, stream)
+    w, wt = _weight(weight, dt, hidden, dev)
+    a = FoldNormGradArgs(
+        rows, hidden, _matrix(dout, rows, hidden, es, "dout", dev),
+        _matrix(sum, rows, hidden, es, "sum", dev), _matrix(dsum, rows, hidden, es, "dsum", dev),
+        _matrix(dx, rows, hidden, es, "dx", dev), w, _floats(rstd, rows, "rstd", dev),
+        _floats(dweight, hidden, "dweight", dev), _ptr(ws),
+        ws.numel() * ws.element_size() if ws is not None else 0, DTYPE[dt], wt)
+    check(L.xred_fold_norm_grad(ctypes.byref(a), _stream(sum, stream)))
