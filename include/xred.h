@@ -485,6 +485,72 @@ XRED_API xred_status xred_fold_norm_grad(const xred_fold_norm_grad_args *args, v
 /* Bytes of workspace xred_fold_norm_grad needs for dweight. */
 XRED_API size_t xred_fold_norm_grad_workspace(uint64_t rows, uint64_t hidden);
 
+/* How xred_route scores an expert. */
+typedef enum { XRED_SCORE_SOFTMAX = 0, XRED_SCORE_SIGMOID = 1 } xred_score;
+enum { XRED_ROUTE_RENORM = 1u };   /* xred_route flags */
+
+/*
+ * Routing of tokens to experts: each token's topk best experts by key, in
+ * descending order, ties to the lowest index.
+ *     softmax   score = softmax(x) over the experts, key = x + bias (the log of
+ *               the score up to a constant of the row)
+ *     sigmoid   score = 1 / (1 + exp(-x)),           key = score + bias
+ * An expert whose logit or whose key is -inf is never chosen; a slot for which
+ * none is left gets id -1 and weight 0 (all of them in a row of -inf, a
+ * padding row).  A NaN key ranks above every number, so that it shows.
+ * With groups > 1 the experts form that many groups of consecutive ones, and
+ * only the group_topk best groups (ties to the lowest) are chosen from; a
+ * group's rank is its best key (group_score 1) or the sum of its best two (2).
+ *     weight    = scale * score; with XRED_ROUTE_RENORM the chosen scores are
+ *                 divided by their sum first (softmax: the softmax over the
+ *                 chosen logits; scores that sum to 0 stay 0)
+ * bias (a balance correction) steers the choice only, not the weights.
+ *   logits   tokens x experts of dtype; bias: experts binary32, or NULL
+ *   ids      tokens x topk int32;  weights: tokens x topk binary32
+ *   experts  1..XRED_MAX_EXPERTS, topk 1..min(experts, XRED_MAX_TOPK), groups
+ *            a divisor of experts up to XRED_MAX_EXPERT_GROUPS, group_topk
+ *            1..groups
+ * Keys are computed in binary32 (x, then exp, + 1, 1 / and + bias, each
+ * rounded), so equal inputs are chosen alike on every call.
+ */
+typedef struct {
+    uint64_t tokens;
+    uint32_t experts, topk;
+    uint32_t groups, group_topk, group_score;
+    uint32_t flags;
+    xred_rows logits;
+    const float *bias;
+    int32_t *ids;
+    float *weights;
+    xred_dtype dtype;
+    xred_score score;
+    float scale;
+} xred_route_args;
+XRED_API xred_status xred_route(const xred_route_args *args, void *hip_stream);
+
+/*
+ * The gradient of xred_route's weights with respect to the logits (the choice
+ * itself and the bias have none): every element of dlogits is written, zero
+ * where the weights do not depend on it.
+ *   ids       as xred_route gave them; ids outside [0, experts) are passed over,
+ *             the others of a token differ
+ *   dweights  tokens x topk binary32
+ *   dlogits   tokens x experts of dtype
+ * score, flags and scale as in the forward call.
+ */
+typedef struct {
+    uint64_t tokens;
+    uint32_t experts, topk;
+    uint32_t flags;
+    xred_rows logits, dlogits;
+    const int32_t *ids;
+    const float *dweights;
+    xred_dtype dtype;
+    xred_score score;
+    float scale;
+} xred_route_grad_args;
+XRED_API xred_status xred_route_grad(const xred_route_grad_args *args, void *hip_stream);
+
 /*
  * CU budget: at most max_workgroups workgroups per launch of the fused,
  * reduce-scatter, step-wise, cast and batched kernels (0 = no limit, the

@@ -60,12 +60,21 @@ FoldNormArgs = _struct("FoldNormArgs", [
 FoldNormGradArgs = _struct("FoldNormGradArgs", [
     "q rows hidden", "r dout sum dsum dx", "p weight rstd dweight workspace",
     "q workspace_bytes", "i dtype weight_dtype"])
+RouteArgs = _struct("RouteArgs", [
+    "q tokens", "u experts topk groups group_topk group_score flags", "r logits",
+    "p bias ids weights", "i dtype score", "f scale"])
+RouteGradArgs = _struct("RouteGradArgs", [
+    "q tokens", "u experts topk flags", "r logits dlogits", "p ids dweights", "i dtype score",
+    "f scale"])
+SCORE = {"softmax": 0, "sigmoid": 1}
+ROUTE_RENORM = 1
 
 EXPORTS = ("xred_allreduce_local", "xred_reduce_scatter_local", "xred_reduce_copy_step",
            "xred_acc_cast", "xred_batched_reduce", "xred_batched_reduce_noalloc",
            "xred_ring_reduce", "xred_ring_max_count",
            "xred_allreduce_sim", "xred_sim_chunk",
            "xred_fold_norm", "xred_fold_norm_grad", "xred_fold_norm_grad_workspace",
+           "xred_route", "xred_route_grad",
            "xred_set_max_workgroups",
            "xred_stream_create_partition", "xred_stream_destroy", "xred_acc_elem_size",
            "xred_status_string",
@@ -120,7 +129,7 @@ def load(path: Path = LIB_PATH) -> ctypes.CDLL:
         getattr(L, f).restype = ctypes.c_int
     L.xred_stream_create_partition.argtypes = [i32, ctypes.POINTER(vp), ctypes.POINTER(vp)]
     L.xred_stream_destroy.argtypes = [vp]
-    for f in ("xred_fold_norm", "xred_fold_norm_grad"):
+    for f in ("xred_fold_norm", "xred_fold_norm_grad", "xred_route", "xred_route_grad"):
         getattr(L, f).argtypes = [vp, vp]
         getattr(L, f).restype = ctypes.c_int
     L.xred_fold_norm_grad_workspace.argtypes = [ctypes.c_uint64, ctypes.c_uint64]

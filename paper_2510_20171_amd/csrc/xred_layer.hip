@@ -1,5 +1,5 @@
 // xred_layer.hip -- the C ABI of the calls around a reduced activation:
-// argument checks and dispatch to the launchers (xred_norm.hip).  As
+// argument checks and dispatch to the launchers (xred_norm.hip, xred_route.hip).  As
 // elsewhere, everything is checked before anything is enqueued.
 #include "xred_layer.hpp"
 
@@ -66,6 +66,25 @@ xred_status check_apart(const Matrix *out, const char *const *names, int nout, c
             if (rows_overlap(out[i], out[j], false))
                 return fail(XRED_ALIAS, "%s overlaps %s", names[i], names[j]);
     }
+    return XRED_SUCCESS;
+}
+
+// What xred_route and its gradient share.
+xred_status check_route(xred_dtype dtype, xred_score score, uint32_t flags, uint32_t experts,
+                        uint32_t topk, uint64_t tokens)
+{
+    if (!row_type(dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)dtype);
+    if (score != XRED_SCORE_SOFTMAX && score != XRED_SCORE_SIGMOID)
+        return fail(XRED_INVALID_ARGUMENT, "unknown score %d", (int)score);
+    if (flags & ~(unsigned)XRED_ROUTE_RENORM)
+        return fail(XRED_INVALID_ARGUMENT, "unknown flag bits 0x%x", flags);
+    if (experts < 1 || experts > XRED_MAX_EXPERTS)
+        return fail(XRED_UNSUPPORTED, "experts = %u outside 1..%d", experts, XRED_MAX_EXPERTS);
+    if (topk < 1 || topk > experts || topk > XRED_MAX_TOPK)
+        return fail(topk >= 1 && topk <= experts ? XRED_UNSUPPORTED : XRED_INVALID_ARGUMENT,
+                    "topk = %u outside 1..min(experts = %u, %d)", topk, experts, XRED_MAX_TOPK);
+    if (tokens > (uint64_t)INT64_MAX / (4 * XRED_MAX_TOPK))
+        return fail(XRED_INVALID_ARGUMENT, "tokens * topk overflows");
     return XRED_SUCCESS;
 }
 
@@ -180,6 +199,60 @@ XRED_API xred_status xred_fold_norm_grad(const xred_fold_norm_grad_args *args, v
     TRY(check_apart(out, names, nout, in, nin, may));
     const hipError_t e = launch_fold_norm_grad(a, (hipStream_t)hip_stream);
     return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "fold_norm_grad launch");
+}
+
+XRED_API xred_status xred_route(const xred_route_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_route_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_route tokens=%llu experts=%u topk=%u groups=%u score=%d dtype=%d "
+                     "stream=%p", (unsigned long long)a.tokens, a.experts, a.topk, a.groups,
+                     (int)a.score, (int)a.dtype, hip_stream);
+    TRY(check_route(a.dtype, a.score, a.flags, a.experts, a.topk, a.tokens));
+    if (a.groups < 1 || a.groups > XRED_MAX_EXPERT_GROUPS || a.experts % a.groups != 0)
+        return fail(XRED_INVALID_ARGUMENT, "groups = %u: not a divisor of %u experts up to %d",
+                    a.groups, a.experts, XRED_MAX_EXPERT_GROUPS);
+    if (a.groups > 1 && (a.group_topk < 1 || a.group_topk > a.groups))
+        return fail(XRED_INVALID_ARGUMENT, "group_topk = %u outside 1..%u", a.group_topk, a.groups);
+    if (a.groups > 1 && a.group_score != 1 && a.group_score != 2)
+        return fail(XRED_INVALID_ARGUMENT, "group_score = %u is neither 1 nor 2", a.group_score);
+    if (a.tokens == 0) return XRED_SUCCESS;
+    Matrix in[2], out[2];
+    const char *const names[2] = {"ids", "weights"};
+    const int may[2] = {0, 0};
+    int nin = 0;
+    TRY(check_rows(a.logits, a.tokens, a.experts, elem_size(a.dtype), "logits", &in[nin++]));
+    if (a.bias)
+        TRY(check_rows(xred_rows{(void *)a.bias, a.experts}, 1, a.experts, 4, "bias", &in[nin++]));
+    TRY(check_rows(xred_rows{a.ids, a.topk}, a.tokens, a.topk, 4, "ids", &out[0]));
+    TRY(check_rows(xred_rows{a.weights, a.topk}, a.tokens, a.topk, 4, "weights", &out[1]));
+    TRY(check_apart(out, names, 2, in, nin, may));
+    const hipError_t e = launch_route(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "route launch");
+}
+
+XRED_API xred_status xred_route_grad(const xred_route_grad_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_route_grad_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_route_grad tokens=%llu experts=%u topk=%u score=%d dtype=%d stream=%p",
+                     (unsigned long long)a.tokens, a.experts, a.topk, (int)a.score, (int)a.dtype,
+                     hip_stream);
+    TRY(check_route(a.dtype, a.score, a.flags, a.experts, a.topk, a.tokens));
+    if (a.tokens == 0) return XRED_SUCCESS;
+    const uint64_t es = elem_size(a.dtype);
+    Matrix in[3], out[1];
+    const char *const names[1] = {"dlogits"};
+    const int may[1] = {0};
+    TRY(check_rows(a.logits, a.tokens, a.experts, es, "logits", &in[0]));
+    TRY(check_rows(xred_rows{(void *)a.ids, a.topk}, a.tokens, a.topk, 4, "ids", &in[1]));
+    TRY(check_rows(xred_rows{(void *)a.dweights, a.topk}, a.tokens, a.topk, 4, "dweights", &in[2]));
+    TRY(check_rows(a.dlogits, a.tokens, a.experts, es, "dlogits", &out[0]));
+    TRY(check_apart(out, names, 1, in, 3, may));
+    const hipError_t e = launch_route_grad(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "route_grad launch");
 }
 
 }  // extern "C"

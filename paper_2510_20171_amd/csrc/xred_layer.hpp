@@ -13,4 +13,7 @@ hipError_t launch_fold_norm(const xred_fold_norm_args &a, hipStream_t stream);
 uint32_t norm_grad_slices(uint64_t rows);
 hipError_t launch_fold_norm_grad(const xred_fold_norm_grad_args &a, hipStream_t stream);
 
+hipError_t launch_route(const xred_route_args &a, hipStream_t stream);
+hipError_t launch_route_grad(const xred_route_grad_args &a, hipStream_t stream);
+
 }  // namespace xred

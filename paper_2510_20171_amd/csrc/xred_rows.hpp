@@ -136,10 +136,12 @@ __device__ __forceinline__ void store_piece_e4m3(char *base, uint32_t off, uint3
 }
 
 // ------------------------------------------------------------- reductions --
-// x of the lane l ^ M, as seen by lane l (M a power of two below 64).
-template <int M>
-__device__ __forceinline__ float lane_xor(float x)
+// x of the lane l ^ M, as seen by lane l (M a power of two below 64; every lane
+// of the wave takes part).
+template <int M, class X>
+__device__ __forceinline__ X lane_xor(X x)
 {
+    static_assert(sizeof(X) == 4, "one register");
     const int v = __builtin_bit_cast(int, x);
     int r;
     if constexpr (M == 1) r = __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true);        // quad 1 0 3 2
@@ -147,7 +149,7 @@ __device__ __forceinline__ float lane_xor(float x)
     else if constexpr (M == 8) r = __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true);  // row_ror 8
     else if constexpr (M == 16 || M == 4) r = __builtin_amdgcn_ds_swizzle(v, (M << 10) | 0x1F);
     else r = __shfl_xor(v, 32);
-    return __builtin_bit_cast(float, r);
+    return __builtin_bit_cast(X, r);
 }
 
 // A sum and a maximum (NaN-propagating, like every maximum here) over aligned
@@ -166,6 +168,26 @@ __device__ __forceinline__ float lanes_max(float x)
     if constexpr (M < N)
         return lanes_max<N, 2 * M>(__builtin_elementwise_maximum(x, lane_xor<M>(x)));
     else return x;
+}
+
+template <int N, int M = 1>
+__device__ __forceinline__ int lanes_max(int x)
+{
+    if constexpr (M < N) {
+        const int y = lane_xor<M>(x);
+        return lanes_max<N, 2 * M>(x > y ? x : y);
+    } else {
+        return x;
+    }
+}
+
+// Orders a wave's LDS accesses before it against those after it, for lanes that
+// read what other lanes of their wave wrote.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 }  // namespace xred

@@ -14,8 +14,9 @@ from __future__ import annotations
 import ctypes
 
 from . import _dtype_name, _ptr, _require, _stream
-from ._lib import (DTYPE, ELEM_SIZE, INVALID_ARGUMENT, FoldNormArgs, FoldNormGradArgs, XredError,
-                   XredRows, check, load, ptr_array)
+from ._lib import (DTYPE, ELEM_SIZE, INVALID_ARGUMENT, ROUTE_RENORM, SCORE, FoldNormArgs,
+                   FoldNormGradArgs, RouteArgs, RouteGradArgs, XredError, XredRows, check, load,
+                   ptr_array)
 
 
 def _refuse(text):
@@ -55,6 +56,21 @@ def _floats(t, n, what, device):
     if t is not None and _dtype_name(t, None) != "f32":
         _refuse(f"{what} is {t.dtype}, expected float32")
     return _vector(t, n, 4, what, device)
+
+
+def _slots(t, rows, topk, what, device, dtypes):
+    """A contiguous tokens x topk tensor of one of `dtypes`, as a pointer."""
+    if _dtype_name(t, None) not in dtypes:
+        _refuse(f"{what} is {t.dtype}, expected {' or '.join(dtypes)}")
+    if tuple(t.shape) != (rows, topk):
+        _refuse(f"{what} has shape {tuple(t.shape)}, expected {(rows, topk)}")
+    return _vector(t, rows * topk, 4, what, device)
+
+
+def _score(name):
+    if name not in SCORE:
+        _refuse(f"unknown score {name!r}")
+    return SCORE[name]
 
 
 def _weight(t, dtype, n, device):
@@ -141,3 +157,42 @@ def fold_norm_grad(dout, sum, rstd, dx, *, weight=None, dsum=None, dweight=None,
         _floats(dweight, hidden, "dweight", dev), _ptr(ws),
         ws.numel() * ws.element_size() if ws is not None else 0, DTYPE[dt], wt)
     check(L.xred_fold_norm_grad(ctypes.byref(a), _stream(sum, stream)))
+
+
+def route(logits, ids, weights, *, score: str = "softmax", bias=None, groups: int = 1,
+          group_topk: int = 1, group_score: int = 2, renorm: bool = True, scale: float = 1.0,
+          stream=None) -> None:
+    """Each token's best experts and their weights (xred_route).
+
+    logits: tokens x experts; ids (int32) and weights (fp32): tokens x topk,
+    best first, ids -1 and weight 0 where no expert is left.  score: "softmax" or
+    "sigmoid"; bias (fp32, one an expert) steers the choice only; with groups > 1
+    the group_topk best groups of experts are chosen from, ranked by their best
+    key (group_score = 1) or their best two."""
+    tokens, experts = _shape(logits, "logits")
+    topk = _shape(ids, "ids")[1]
+    dt, dev = _dtype_name(logits, None), logits.device
+    a = RouteArgs(
+        tokens, experts, topk, groups, group_topk, group_score, ROUTE_RENORM if renorm else 0,
+        _matrix(logits, tokens, experts, ELEM_SIZE[dt], "logits", dev),
+        _floats(bias, experts, "bias", dev), _slots(ids, tokens, topk, "ids", dev, ("i32",)),
+        _slots(weights, tokens, topk, "weights", dev, ("f32",)), DTYPE[dt], _score(score), scale)
+    check(load().xred_route(ctypes.byref(a), _stream(logits, stream)))
+
+
+def route_grad(logits, ids, dweights, dlogits, *, score: str = "softmax", renorm: bool = True,
+               scale: float = 1.0, stream=None) -> None:
+    """The gradient of route's weights with respect to the logits (xred_route_grad)."""
+    tokens, experts = _shape(logits, "logits")
+    topk = _shape(ids, "ids")[1]
+    dt, dev = _dtype_name(logits, None), logits.device
+    if dlogits.dtype != logits.dtype:
+        _refuse(f"dlogits is {dlogits.dtype}, logits is {logits.dtype}")
+    es = ELEM_SIZE[dt]
+    a = RouteGradArgs(
+        tokens, experts, topk, ROUTE_RENORM if renorm else 0,
+        _matrix(logits, tokens, experts, es, "logits", dev),
+        _matrix(dlogits, tokens, experts, es, "dlogits", dev),
+        _slots(ids, tokens, topk, "ids", dev, ("i32",)),
+        _slots(dweights, tokens, topk, "dweights", dev, ("f32",)), DTYPE[dt], _score(score), scale)
+    check(load().xred_route_grad(ctypes.byref(a), _stream(logits, stream)))
