@@ -552,6 +552,94 @@ typedef struct {
 XRED_API xred_status xred_route_grad(const xred_route_grad_args *args, void *hip_stream);
 
 /*
+ * Order of the routed rows by expert.  Slot j of token t (index t * topk + j)
+ * with expert ids[t][j] in [0, experts) becomes row
+ *     pos[t][j] = offsets[id] + the number of earlier slots of that expert
+ * of the dispatched rows; any other id drops the slot, and its pos is -1.
+ *   ids      tokens x topk int32;  pos: the same shape, output
+ *   counts   experts int32, output: rows of each expert
+ *   offsets  experts + 1 int32, output: each expert's first row, then the
+ *            number of rows in all
+ *   slots    optional output, tokens * topk int32: the slot of every row, for
+ *            rows 0..offsets[experts] - 1 (later entries are left untouched)
+ *   experts  1..XRED_MAX_EXPERTS, topk 1..XRED_MAX_TOPK (else
+ *            XRED_UNSUPPORTED), tokens * topk below 2^31
+ * No tokens: counts and offsets are set to 0.
+ */
+typedef struct {
+    uint64_t tokens;
+    uint32_t experts, topk;
+    const int32_t *ids;
+    int32_t *counts, *offsets, *pos, *slots;
+    void *workspace;
+    uint64_t workspace_bytes;
+} xred_dispatch_plan_args;
+XRED_API xred_status xred_dispatch_plan(const xred_dispatch_plan_args *args, void *hip_stream);
+
+/* Bytes of workspace xred_dispatch_plan needs for tokens * topk = slots; 0 where
+ * it needs none (small batches). */
+XRED_API size_t xred_dispatch_plan_workspace(uint64_t slots, uint32_t experts);
+
+/*
+ * Rows to their places: out[pos[t][j]] = x[t] for every slot whose pos is in
+ * [0, out_rows); other slots are passed over, and rows no slot names are left
+ * untouched.  Bits are copied (any dtype).
+ *   x          tokens x hidden;  out: out_rows x hidden, both of dtype
+ *   scale, out_scale   optional, together: tokens x scale_columns and out_rows x
+ *              scale_columns binary32 values that travel with the rows (the
+ *              scales of 8-bit rows)
+ *   pos        tokens x topk int32; the places of one call differ
+ */
+typedef struct {
+    uint64_t tokens, hidden, out_rows, scale_columns;
+    uint32_t topk;
+    xred_dtype dtype;
+    xred_rows x, out, scale, out_scale;
+    const int32_t *pos;
+} xred_dispatch_args;
+XRED_API xred_status xred_dispatch(const xred_dispatch_args *args, void *hip_stream);
+
+/*
+ * The experts' rows back to their tokens, a weighted fold in slot order:
+ *     out[t] = down(((up(base[t]) + w[t][0] * up(y[pos[t][0]])) + ...))
+ * over the slots whose pos is in [0, y_rows); without base the fold starts from
+ * the first product, and a token without a slot gives base, or 0.  Without
+ * weights w is 1 (with them left out it is also the gradient of xred_dispatch).
+ *   y        y_rows x hidden;  base (optional), out: tokens x hidden, of dtype;
+ *            out may be base (the same pointer and stride)
+ *   weights  tokens x topk binary32, or NULL;  pos: tokens x topk int32
+ */
+typedef struct {
+    uint64_t tokens, hidden, y_rows;
+    uint32_t topk;
+    xred_dtype dtype;
+    xred_rows y, base, out;
+    const int32_t *pos;
+    const float *weights;
+} xred_combine_args;
+XRED_API xred_status xred_combine(const xred_combine_args *args, void *hip_stream);
+
+/*
+ * The gradient of xred_combine (base's is dout itself):
+ *     dy[pos[t][j]]  = down(w[t][j] * up(dout[t]))
+ *     dweights[t][j] = sum over the row of up(dout[t]) * up(y[pos[t][j]])
+ * for the slots whose pos is in [0, y_rows), whose places differ; the others'
+ * dweights are 0, and rows of dy no slot names are left untouched.
+ *   dweights  tokens x topk binary32, optional (y is then not read)
+ *   dy        may be y (the same pointer and stride)
+ */
+typedef struct {
+    uint64_t tokens, hidden, y_rows;
+    uint32_t topk;
+    xred_dtype dtype;
+    xred_rows dout, y, dy;
+    const int32_t *pos;
+    const float *weights;
+    float *dweights;
+} xred_combine_grad_args;
+XRED_API xred_status xred_combine_grad(const xred_combine_grad_args *args, void *hip_stream);
+
+/*
  * CU budget: at most max_workgroups workgroups per launch of the fused,
  * reduce-scatter, step-wise, cast and batched kernels (0 = no limit, the
  * default), so a reduction can run beside compute kernels on the rest of the

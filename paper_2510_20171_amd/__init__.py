@@ -31,6 +31,7 @@ __all__ = ["allreduce_local", "reduce_scatter_local", "reduce_copy_step", "acc_c
            "batched_reduce", "ring_reduce", "ring_max_count", "allreduce_sim", "sim_chunk",
            "set_max_workgroups", "stream_create_partition", "stream_destroy", "pack_items", "acc_elem_size", "version", "release",
            "fold_norm", "fold_norm_grad", "route", "route_grad",
+           "dispatch_plan", "dispatch", "combine", "combine_grad",
            "XredError", "load", "EXPORTS"]
 
 
@@ -300,4 +301,5 @@ def release() -> None:
     load().xred_release()
 
 
-from .layer import fold_norm, fold_norm_grad, route, route_grad  # noqa: E402  (they use the helpers above)
+from .layer import (combine, combine_grad, dispatch, dispatch_plan, fold_norm,  # noqa: E402
+                    fold_norm_grad, route, route_grad)   # they use the helpers above

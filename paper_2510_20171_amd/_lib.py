@@ -66,6 +66,15 @@ RouteArgs = _struct("RouteArgs", [
 RouteGradArgs = _struct("RouteGradArgs", [
     "q tokens", "u experts topk flags", "r logits dlogits", "p ids dweights", "i dtype score",
     "f scale"])
+DispatchPlanArgs = _struct("DispatchPlanArgs", [
+    "q tokens", "u experts topk", "p ids counts offsets pos slots workspace", "q workspace_bytes"])
+DispatchArgs = _struct("DispatchArgs", [
+    "q tokens hidden out_rows scale_columns", "u topk", "i dtype", "r x out scale out_scale",
+    "p pos"])
+CombineArgs = _struct("CombineArgs", [
+    "q tokens hidden y_rows", "u topk", "i dtype", "r y base out", "p pos weights"])
+CombineGradArgs = _struct("CombineGradArgs", [
+    "q tokens hidden y_rows", "u topk", "i dtype", "r dout y dy", "p pos weights dweights"])
 SCORE = {"softmax": 0, "sigmoid": 1}
 ROUTE_RENORM = 1
 
@@ -75,6 +84,8 @@ EXPORTS = ("xred_allreduce_local", "xred_reduce_scatter_local", "xred_reduce_cop
            "xred_allreduce_sim", "xred_sim_chunk",
            "xred_fold_norm", "xred_fold_norm_grad", "xred_fold_norm_grad_workspace",
            "xred_route", "xred_route_grad",
+           "xred_dispatch_plan", "xred_dispatch_plan_workspace", "xred_dispatch",
+           "xred_combine", "xred_combine_grad",
            "xred_set_max_workgroups",
            "xred_stream_create_partition", "xred_stream_destroy", "xred_acc_elem_size",
            "xred_status_string",
@@ -129,11 +140,14 @@ def load(path: Path = LIB_PATH) -> ctypes.CDLL:
         getattr(L, f).restype = ctypes.c_int
     L.xred_stream_create_partition.argtypes = [i32, ctypes.POINTER(vp), ctypes.POINTER(vp)]
     L.xred_stream_destroy.argtypes = [vp]
-    for f in ("xred_fold_norm", "xred_fold_norm_grad", "xred_route", "xred_route_grad"):
+    for f in ("xred_fold_norm", "xred_fold_norm_grad", "xred_route", "xred_route_grad",
+              "xred_dispatch_plan", "xred_dispatch", "xred_combine", "xred_combine_grad"):
         getattr(L, f).argtypes = [vp, vp]
         getattr(L, f).restype = ctypes.c_int
     L.xred_fold_norm_grad_workspace.argtypes = [ctypes.c_uint64, ctypes.c_uint64]
     L.xred_fold_norm_grad_workspace.restype = sz
+    L.xred_dispatch_plan_workspace.argtypes = [ctypes.c_uint64, ctypes.c_uint32]
+    L.xred_dispatch_plan_workspace.restype = sz
     L.xred_set_max_workgroups.argtypes = [ctypes.c_uint]
     L.xred_set_max_workgroups.restype = ctypes.c_uint
     L.xred_acc_elem_size.argtypes = [i32]

@@ -1,0 +1,581 @@
+// xred_experts.hip -- rows to experts and back: the order of rows by expert
+// (xred_dispatch_plan), the rows' copies (xred_dispatch), their weighted
+// reduction to tokens (xred_combine) and its gradient (xred_combine_grad).
+#include "xred_layer.hpp"
+#include "xred_rows.hpp"
+
+namespace xred {
+namespace {
+
+// -------------------------------------------------------------------- plan --
+// A stable counting sort of the slots by expert.  A workgroup takes a range of
+// consecutive slots, kPlanTile at a time, each wave a run of them in order: the
+// lanes of a wave that share an expert find each other by ballots over the
+// expert's bits, so a slot's place among its wave's is a population count, and
+// no atomic decides an order.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kPlanSteps = 4;
+constexpr uint32_t kPlanTile = kPlanThreads * kPlanSteps;
+// Up to this many slots one workgroup plans alone (one launch); beyond, a first
+// launch counts, and each workgroup of the second adds up what lies before it.
+constexpr uint32_t kPlanAlone = 4 * kPlanTile;
+constexpr uint32_t kPlanMostWgs = 128;
+
+struct PlanParams {
+    const int32_t *ids;
+    int32_t *counts, *offsets, *pos, *slots;
+    uint32_t *parts;            // [wgs][experts], or NULL (one workgroup)
+    uint32_t n, experts, wgs;   // slots; workgroups that share them
+    uint32_t range;             // slots of a workgroup, a multiple of kPlanTile
+};
+
+// Counts of the experts among slots [lo, hi) into hist[experts] (LDS, cleared
+// here); ends with a barrier.
+__device__ __forceinline__ void plan_count(const PlanParams &p, uint32_t lo, uint32_t hi,
+                                           uint32_t *hist)
+{
+    for (uint32_t e = threadIdx.x; e < p.experts; e += kPlanThreads) hist[e] = 0;
+    __syncthreads();
+    for (uint32_t i = lo + threadIdx.x; i < hi; i += kPlanThreads) {
+        const uint32_t e = (uint32_t)p.ids[i];
+        if (e < p.experts) atomicAdd(&hist[e], 1u);   // integers: any order
+    }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(PlanParams p)
+{
+    __shared__ uint32_t hist[XRED_MAX_EXPERTS];
+    for (uint32_t b = blockIdx.x; b < p.wgs; b += gridDim.x) {
+        const uint32_t lo = b * p.range, hi = p.n - lo < p.range ? p.n : lo + p.range;
+        plan_count(p, lo, hi, hist);
+        for (uint32_t e = threadIdx.x; e < p.experts; e += kPlanThreads)
+            p.parts[b * p.experts + e] = hist[e];
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanParams p)
+{
+    __shared__ uint32_t base[XRED_MAX_EXPERTS];   // the next row of each expert
+    __shared__ uint32_t total[XRED_MAX_EXPERTS];
+    __shared__ uint16_t in_wave[kPlanWaves][XRED_MAX_EXPERTS];
+    __shared__ uint32_t wave_total[kPlanWaves];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    for (uint32_t b = blockIdx.x; b < p.wgs; b += gridDim.x) {
+        const uint32_t lo = b * p.range, hi = p.n - lo < p.range ? p.n : lo + p.range;
+        // counts of all slots, and of those before this range
+        if (p.parts == nullptr) {
+            plan_count(p, lo, hi, total);
+            for (uint32_t e = threadIdx.x; e < p.experts; e += kPlanThreads) base[e] = 0;
+        } else {
+            for (uint32_t e = threadIdx.x; e < p.experts; e += kPlanThreads) total[e] = base[e] = 0;
+            __syncthreads();
+            // every thread an expert and some of the workgroups: a column of
+            // `parts` is short, and its loads would wait for one another
+            const uint32_t columns = p.experts <= 64 ? 64 : p.experts <= 256 ? 256 : kPlanThreads;
+            const uint32_t e = threadIdx.x % columns, share = kPlanThreads / columns;
+            if (e < p.experts) {
+                uint32_t all = 0, before = 0;
+#pragma unroll 4
+                for (uint32_t i = threadIdx.x / columns; i < p.wgs; i += share) {
+                    const uint32_t c = p.parts[i * p.experts + e];
+                    all += c;
+                    before += i < b ? c : 0;
+                }
+                atomicAdd(&total[e], all);
+                atomicAdd(&base[e], before);
+            }
+        }
+        __syncthreads();
+        // offsets: an exclusive scan over the experts, one a thread
+        static_assert(XRED_MAX_EXPERTS <= kPlanThreads, "one expert a thread");
+        const uint32_t c = threadIdx.x < p.experts ? total[threadIdx.x] : 0;
+        uint32_t sum = c;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t x = __shfl_up(sum, d);
+            sum += (int)lane >= d ? x : 0;
+        }
+        if (lane == 63) wave_total[wave] = sum;
+        __syncthreads();
+        uint32_t first = sum - c;
+        for (uint32_t w = 0; w < wave; ++w) first += wave_total[w];
+        if (threadIdx.x < p.experts) base[threadIdx.x] += first;
+        if (b == 0 && threadIdx.x < p.experts) {
+            p.counts[threadIdx.x] = (int32_t)c;
+            p.offsets[threadIdx.x] = (int32_t)first;
+            if (threadIdx.x == p.experts - 1) p.offsets[p.experts] = (int32_t)(first + c);
+        }
+        const uint32_t bits = 32 - __clz(p.experts);   // of an id, experts for "none" included
+        for (uint32_t at = lo; at < hi; at += kPlanTile) {
+            const uint32_t left = hi - at;
+            // as many steps of a wave as spread what is left over all of them
+            const uint32_t steps = left >= kPlanTile ? kPlanSteps : (left + kPlanThreads - 1) / kPlanThreads;
+            for (uint32_t e = lane; e < p.experts; e += 64) in_wave[wave][e] = 0;
+            uint32_t id[kPlanSteps], rank[kPlanSteps];
+            wave_sync();
+#pragma unroll
+            for (int s = 0; s < kPlanSteps; ++s) {
+                const uint32_t i = (wave * steps + s) * 64 + lane;
+                const bool on = s < (int)steps && i < left;
+                id[s] = on ? (uint32_t)p.ids[at + i] : p.experts;
+                if (id[s] > p.experts) id[s] = p.experts;
+            }
+#pragma unroll
+            for (int s = 0; s < kPlanSteps; ++s) {
+                rank[s] = 0;
+                if (s < (int)steps) {
+                    uint64_t same = ~0ull;
+                    for (uint32_t k = 0; k < bits; ++k) {
+                        const bool set = (id[s] >> k) & 1;
+                        const uint64_t those = __builtin_amdgcn_ballot_w64(set);
+                        same &= set ? those : ~those;
+                    }
+                    const uint32_t below = __popcll(same & ((1ull << lane) - 1));
+                    if (id[s] < p.experts) {
+                        const uint32_t earlier = in_wave[wave][id[s]];
+                        rank[s] = earlier + below;
+                    }
+                    wave_sync();   // all have read before the first of each expert counts up
+                    if (id[s] < p.experts && below == 0)
+                        in_wave[wave][id[s]] = (uint16_t)(rank[s] + __popcll(same));
+                    wave_sync();
+                }
+            }
+            __syncthreads();
+            // each wave's first row of each expert, relative to base
+            const uint32_t e = threadIdx.x;
+            uint32_t tile = 0;
+            if (e < p.experts)
+                for (int w = 0; w < kPlanWaves; ++w) {
+                    const uint32_t x = in_wave[w][e];
+                    in_wave[w][e] = (uint16_t)tile;
+                    tile += x;
+                }
+            __syncthreads();
+#pragma unroll
+            for (int s = 0; s < kPlanSteps; ++s) {
+                const uint32_t i = (wave * steps + s) * 64 + lane;
+                if (s < (int)steps && i < left) {
+                    const bool on = id[s] < p.experts;
+                    const uint32_t row = on ? base[id[s]] + in_wave[wave][id[s]] + rank[s] : 0;
+                    p.pos[at + i] = on ? (int32_t)row : -1;
+                    if (on && p.slots) p.slots[row] = (int32_t)(at + i);
+                }
+            }
+            __syncthreads();
+            if (e < p.experts) base[e] += tile;
+        }
+        __syncthreads();
+    }
+}
+
+uint32_t plan_wgs(uint64_t n)
+{
+    if (n <= kPlanAlone) return 1;
+    const uint64_t tiles = (n + kPlanTile - 1) / kPlanTile;
+    return (uint32_t)(tiles < kPlanMostWgs ? tiles : kPlanMostWgs);
+}
+
+// ------------------------------------------------------------ work by waves --
+// Rows are cut into column tiles of 64 lanes; a wave takes (token, tile) items,
+// tile by tile within a token, so a launch has enough waves with few tokens and
+// neighbouring waves share rows.
+constexpr int kItemWaves = 4;
+constexpr uint32_t kMostItemWgs = 1u << 20;   // an item's number fits 32 bits
+
+struct Items {
+    uint64_t tokens;
+    uint32_t tiles;                    // of a row
+    uint32_t step_tokens, step_tiles;  // from an item to the wave's next one
+};
+
+struct Item {
+    uint64_t token;
+    uint32_t tile;
+    __device__ __forceinline__ explicit Item(const Items &s)
+    {
+        const uint32_t i =
+            blockIdx.x * kItemWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        token = i / s.tiles;
+        tile = i % s.tiles;
+    }
+    __device__ __forceinline__ void next(const Items &s)
+    {
+        token += s.step_tokens;
+        tile += s.step_tiles;
+        if (tile >= s.tiles) {
+            tile -= s.tiles;
+            ++token;
+        }
+    }
+};
+
+unsigned plan_items(Items &s, uint64_t tokens, uint64_t tiles)
+{
+    s.tokens = tokens;
+    s.tiles = (uint32_t)tiles;
+    const unsigned __int128 items = (unsigned __int128)tokens * tiles;
+    const uint64_t wgs = items > (uint64_t)kMostItemWgs * kItemWaves
+                             ? kMostItemWgs
+                             : ((uint64_t)items + kItemWaves - 1) / kItemWaves;
+    const unsigned grid = grid_for(wgs);
+    s.step_tokens = (uint32_t)((uint64_t)grid * kItemWaves / tiles);
+    s.step_tiles = (uint32_t)((uint64_t)grid * kItemWaves % tiles);
+    return grid;
+}
+
+// ---------------------------------------------------------------- dispatch --
+struct DispatchParams {
+    Items items;
+    const char *x;
+    char *out;
+    const float *scale;
+    float *out_scale;
+    const int32_t *pos;
+    uint64_t out_rows;
+    uint64_t stride, out_stride;               // bytes
+    uint64_t scale_stride, out_scale_stride;   // elements
+    uint32_t bytes, topk, scale_columns;
+};
+
+constexpr int kCopyVecs = 2;   // vectors a lane of a tile
+
+// A row is read once and written topk times.  Its last vector ends with the row,
+// overlapping the one before it (both write the same bytes there), so there is
+// no tail but in rows shorter than a vector.
+__global__ __launch_bounds__(64 * kItemWaves) void dispatch_kernel(DispatchParams p)
+{
+    const uint32_t lane = threadIdx.x % 64;
+    const uint32_t vecs = (p.bytes + 15) / 16;
+    for (Item it(p.items); it.token < p.items.tokens; it.next(p.items)) {
+        const char *x = p.x + it.token * p.stride;
+        const int32_t *pos = p.pos + it.token * p.topk;
+        u32x4 v[kCopyVecs];
+        uint32_t off[kCopyVecs];
+        bool on[kCopyVecs];
+#pragma unroll
+        for (int u = 0; u < kCopyVecs; ++u) {
+            const uint32_t i = (it.tile * kCopyVecs + u) * 64 + lane;
+            on[u] = i < vecs && p.bytes >= 16;
+            off[u] = i + 1 < vecs ? 16 * i : p.bytes - 16;
+            if (on[u])
+                v[u] = __builtin_nontemporal_load(
+                    (const __attribute__((address_space(1))) u32x4_any *)((global_bytes)x + off[u]));
+        }
+        for (uint32_t j = 0; j < p.topk; ++j) {
+            const int32_t to = sload(pos + j);
+            if (to < 0 || (uint64_t)to >= p.out_rows) continue;
+            char *out = p.out + (uint64_t)to * p.out_stride;
+#pragma unroll
+            for (int u = 0; u < kCopyVecs; ++u)
+                if (on[u])
+                    *(__attribute__((address_space(1))) u32x4_any *)((global_out)out + off[u]) = v[u];
+            if (p.bytes < 16 && lane < p.bytes) out[lane] = x[lane];
+            if (it.tile == 0 && p.scale) {
+                const float *s = p.scale + it.token * p.scale_stride;
+                float *o = p.out_scale + (uint64_t)to * p.out_scale_stride;
+                for (uint32_t c = lane; c < p.scale_columns; c += 64) o[c] = s[c];
+            }
+        }
+    }
+}
+
+// ----------------------------------------------------------------- combine --
+struct CombineParams {
+    Items items;
+    const char *y, *base;
+    char *out;
+    const int32_t *pos;
+    const float *weights;
+    uint64_t y_rows;
+    uint64_t y_stride, base_stride, out_stride;   // bytes
+    uint32_t hidden, topk;
+};
+
+constexpr int kCombineSlots = 8;   // rows whose loads are in flight together
+
+// One piece a lane.  Bound by HBM: k rows are read for one that is written.
+template <class T>
+__global__ __launch_bounds__(64 * kItemWaves) void combine_kernel(CombineParams p)
+{
+    const uint32_t lane = threadIdx.x % 64;
+    for (Item it(p.items); it.token < p.items.tokens; it.next(p.items)) {
+        const uint32_t piece = it.tile * 64 + lane, c = piece_count(piece, p.hidden);
+        const uint32_t off = piece * 8 * T::kSize, whole = c == 8 ? off : 0;
+        const int32_t *pos = p.pos + it.token * p.topk;
+        const float *weights = p.weights ? p.weights + it.token * p.topk : nullptr;
+        const char *base = p.base ? p.base + it.token * p.base_stride : nullptr;
+        // -0 + t is t for every t, so the fold starts from its first term
+        float acc[8];
+        bool any = base != nullptr;
+        auto clear = [&] {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = -0.0f;
+        };
+        auto fold = [&](const float(&x)[8], float w, bool weighted) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += weighted ? w * x[i] : x[i];
+        };
+        clear();
+        if (p.hidden >= 8) {
+            Piece<T> b;
+            if (base) b = load_piece<T>(base, whole);
+            for (uint32_t j0 = 0; j0 < p.topk; j0 += kCombineSlots) {
+                Piece<T> in[kCombineSlots];
+                bool on[kCombineSlots];
+#pragma unroll
+                for (int g = 0; g < kCombineSlots; ++g) {
+                    const int32_t from = j0 + g < p.topk ? sload(pos + j0 + g) : -1;
+                    on[g] = from >= 0 && (uint64_t)from < p.y_rows;
+                    if (on[g]) in[g] = load_piece<T>(p.y + (uint64_t)from * p.y_stride, whole);
+                }
+                if (j0 == 0 && base) {
+                    float x[8];
+                    up_piece<T>(b, x);
+                    fold(x, 1.0f, false);
+                }
+#pragma unroll
+                for (int g = 0; g < kCombineSlots; ++g)
+                    if (on[g]) {
+                        any = true;
+                        float x[8];
+                        up_piece<T>(in[g], x);
+                        fold(x, weights ? sload(weights + j0 + g) : 1.0f, weights != nullptr);
+                    }
+            }
+        }
+        if (c != 0 && c != 8) {   // the row's end, by one lane
+            clear();
+            float x[8];
+            if (base) {
+                up_short<T>(base, off, c, x);
+                fold(x, 1.0f, false);
+            }
+            for (uint32_t j = 0; j < p.topk; ++j) {
+                const int32_t from = pos[j];
+                if (from < 0 || (uint64_t)from >= p.y_rows) continue;
+                any = true;
+                up_short<T>(p.y + (uint64_t)from * p.y_stride, off, c, x);
+                fold(x, weights ? weights[j] : 1.0f, weights != nullptr);
+            }
+        }
+        if (!any)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+        store_piece<T>(p.out + it.token * p.out_stride, off, c, acc);
+    }
+}
+
+struct CombineGradParams {
+    const char *dout, *y;
+    char *dy;
+    const int32_t *pos;
+    const float *weights;
+    float *dweights;
+    uint64_t tokens, y_rows;
+    uint64_t dout_stride, y_stride, dy_stride;   // bytes
+    uint32_t hidden, topk;
+};
+
+// TPR threads a token, RPB tokens a workgroup (a wave each where RPB > 1): dout's
+// pieces are read once for kCombineSlots slots, whose rows' dot products with
+// dout stay in registers until the row's end.
+template <class T, int TPR, int RPB>
+__global__ __launch_bounds__(TPR *RPB) void combine_grad_kernel(CombineGradParams p)
+{
+    constexpr int kWaves = TPR / 64;
+    __shared__ float red[2][kWaves][kCombineSlots];
+    const uint32_t tid = threadIdx.x % TPR;
+    const uint32_t sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
+    const uint32_t pieces = (p.hidden + 7) / 8;
+    int turn = 0;
+    for (uint64_t token = (uint64_t)blockIdx.x * RPB + sub; token < p.tokens;
+         token += (uint64_t)gridDim.x * RPB) {
+        const int32_t *pos = p.pos + token * p.topk;
+        const float *weights = p.weights + token * p.topk;
+        const char *dout = p.dout + token * p.dout_stride;
+        for (uint32_t j0 = 0; j0 < p.topk; j0 += kCombineSlots) {
+            float dot[kCombineSlots], w[kCombineSlots];
+            uint64_t row[kCombineSlots];
+            bool on[kCombineSlots];
+#pragma unroll
+            for (int g = 0; g < kCombineSlots; ++g) {
+                const int32_t at = j0 + g < p.topk ? sload(pos + j0 + g) : -1;
+                on[g] = at >= 0 && (uint64_t)at < p.y_rows;
+                row[g] = on[g] ? (uint64_t)at : 0;
+                w[g] = on[g] ? sload(weights + j0 + g) : 0.0f;
+                dot[g] = 0.0f;
+            }
+            for (uint32_t i = tid; i < pieces; i += TPR) {
+                const uint32_t c = piece_count(i, p.hidden), off = i * 8 * T::kSize;
+                float d[8];
+                if (c == 8) {
+                    Piece<T> in[kCombineSlots];
+                    const Piece<T> a = load_piece<T, true>(dout, off);
+                    if (p.dweights)
+#pragma unroll
+                        for (int g = 0; g < kCombineSlots; ++g)
+                            if (on[g]) in[g] = load_piece<T>(p.y + row[g] * p.y_stride, off);
+                    up_piece<T>(a, d);
+                    if (p.dweights)
+#pragma unroll
+                        for (int g = 0; g < kCombineSlots; ++g)
+                            if (on[g]) {
+                                float x[8];
+                                up_piece<T>(in[g], x);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) dot[g] += d[e] * x[e];
+                            }
+                } else {
+                    up_short<T>(dout, off, c, d);
+                    if (p.dweights)
+#pragma unroll
+                        for (int g = 0; g < kCombineSlots; ++g)
+                            if (on[g]) {
+                                float x[8];
+                                up_short<T>(p.y + row[g] * p.y_stride, off, c, x);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) dot[g] += d[e] * x[e];
+                            }
+                }
+#pragma unroll
+                for (int g = 0; g < kCombineSlots; ++g)
+                    if (on[g]) {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = w[g] * d[e];
+                        store_piece<T>(p.dy + row[g] * p.dy_stride, off, c, x);
+                    }
+            }
+            if (!p.dweights) continue;
+#pragma unroll
+            for (int g = 0; g < kCombineSlots; ++g) dot[g] = lanes_sum<64>(dot[g]);
+            if constexpr (kWaves > 1) {
+                if (tid % 64 == 0)
+#pragma unroll
+                    for (int g = 0; g < kCombineSlots; ++g) red[turn][tid / 64][g] = dot[g];
+                __syncthreads();
+#pragma unroll
+                for (int g = 0; g < kCombineSlots; ++g) {
+                    dot[g] = red[turn][0][g];
+#pragma unroll
+                    for (int k = 1; k < kWaves; ++k) dot[g] += red[turn][k][g];
+                }
+                turn ^= 1;
+            }
+#pragma unroll
+            for (int g = 0; g < kCombineSlots; ++g)
+                if (tid == (uint32_t)g && j0 + g < p.topk)
+                    p.dweights[token * p.topk + j0 + g] = on[g] ? dot[g] : 0.0f;
+        }
+    }
+}
+
+template <class T, int TPR, int RPB>
+hipError_t go_combine_grad(const CombineGradParams &p, hipStream_t s)
+{
+    return launch_kernel(combine_grad_kernel<T, TPR, RPB>,
+                         dim3(grid_for((p.tokens + RPB - 1) / RPB)), dim3(TPR * RPB), 0, s, p);
+}
+
+}  // namespace
+
+uint64_t dispatch_plan_bytes(uint64_t n, uint32_t experts)
+{
+    const uint32_t wgs = plan_wgs(n);
+    return wgs == 1 ? 0 : (uint64_t)wgs * experts * 4;
+}
+
+hipError_t launch_dispatch_plan(const xred_dispatch_plan_args &a, hipStream_t stream)
+{
+    PlanParams p{};
+    p.ids = a.ids;
+    p.counts = a.counts;
+    p.offsets = a.offsets;
+    p.pos = a.pos;
+    p.slots = a.slots;
+    p.n = (uint32_t)(a.tokens * a.topk);
+    p.experts = a.experts;
+    const uint32_t want = plan_wgs(p.n);
+    const uint32_t tiles = (p.n + kPlanTile - 1) / kPlanTile;
+    p.range = tiles == 0 ? kPlanTile : (tiles + want - 1) / want * kPlanTile;
+    p.wgs = p.n == 0 ? 1 : (p.n + p.range - 1) / p.range;
+    p.parts = want == 1 ? nullptr : (uint32_t *)a.workspace;
+    const dim3 grid(grid_for(p.wgs)), block(kPlanThreads);
+    if (p.parts) {
+        const hipError_t e = launch_kernel(plan_count_kernel, grid, block, 0, stream, p);
+        if (e != hipSuccess) return e;
+    }
+    return launch_kernel(plan_place_kernel, grid, block, 0, stream, p);
+}
+
+hipError_t launch_dispatch(const xred_dispatch_args &a, hipStream_t stream)
+{
+    const uint64_t es = elem_size(a.dtype);
+    DispatchParams p{};
+    p.x = (const char *)a.x.data;
+    p.out = (char *)a.out.data;
+    p.scale = (const float *)a.scale.data;
+    p.out_scale = (float *)a.out_scale.data;
+    p.pos = a.pos;
+    p.out_rows = a.out_rows;
+    p.stride = a.x.stride * es;
+    p.out_stride = a.out.stride * es;
+    p.scale_stride = a.scale.stride;
+    p.out_scale_stride = a.out_scale.stride;
+    p.bytes = (uint32_t)(a.hidden * es);
+    p.topk = a.topk;
+    p.scale_columns = (uint32_t)a.scale_columns;
+    constexpr uint64_t tile = 64 * kCopyVecs * 16;
+    const unsigned grid = plan_items(p.items, a.tokens, (p.bytes + tile - 1) / tile);
+    return launch_kernel(dispatch_kernel, dim3(grid), dim3(64 * kItemWaves), 0, stream, p);
+}
+
+hipError_t launch_combine(const xred_combine_args &a, hipStream_t stream)
+{
+    const uint64_t es = elem_size(a.dtype);
+    CombineParams p{};
+    p.y = (const char *)a.y.data;
+    p.base = (const char *)a.base.data;
+    p.out = (char *)a.out.data;
+    p.pos = a.pos;
+    p.weights = a.weights;
+    p.y_rows = a.y_rows;
+    p.y_stride = a.y.stride * es;
+    p.base_stride = a.base.stride * es;
+    p.out_stride = a.out.stride * es;
+    p.hidden = (uint32_t)a.hidden;
+    p.topk = a.topk;
+    const unsigned grid = plan_items(p.items, a.tokens, (a.hidden + 511) / 512);
+    return with_dtype_among<TF32, TBF16, TF16>(a.dtype, [&](auto t) {
+        return launch_kernel(combine_kernel<decltype(t)>, dim3(grid), dim3(64 * kItemWaves), 0,
+                             stream, p);
+    });
+}
+
+hipError_t launch_combine_grad(const xred_combine_grad_args &a, hipStream_t stream)
+{
+    const uint64_t es = elem_size(a.dtype);
+    CombineGradParams p{};
+    p.dout = (const char *)a.dout.data;
+    p.y = (const char *)a.y.data;
+    p.dy = (char *)a.dy.data;
+    p.pos = a.pos;
+    p.weights = a.weights;
+    p.dweights = a.dweights;
+    p.tokens = a.tokens;
+    p.y_rows = a.y_rows;
+    p.dout_stride = a.dout.stride * es;
+    p.y_stride = a.y.stride * es;
+    p.dy_stride = a.dy.stride * es;
+    p.hidden = (uint32_t)a.hidden;
+    p.topk = a.topk;
+    return with_dtype_among<TF32, TBF16, TF16>(a.dtype, [&](auto t) {
+        using T = decltype(t);
+        if (a.hidden <= 512) return go_combine_grad<T, 64, 4>(p, stream);
+        return go_combine_grad<T, 256, 1>(p, stream);
+    });
+}
+
+}  // namespace xred

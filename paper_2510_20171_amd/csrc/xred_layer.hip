@@ -1,6 +1,6 @@
 // xred_layer.hip -- the C ABI of the calls around a reduced activation:
-// argument checks and dispatch to the launchers (xred_norm.hip, xred_route.hip).  As
-// elsewhere, everything is checked before anything is enqueued.
+// argument checks and dispatch to the launchers (xred_norm.hip, xred_route.hip,
+// xred_experts.hip).  As elsewhere, everything is checked before anything is enqueued.
 #include "xred_layer.hpp"
 
 namespace xred {
@@ -86,6 +86,25 @@ xred_status check_route(xred_dtype dtype, xred_score score, uint32_t flags, uint
     if (tokens > (uint64_t)INT64_MAX / (4 * XRED_MAX_TOPK))
         return fail(XRED_INVALID_ARGUMENT, "tokens * topk overflows");
     return XRED_SUCCESS;
+}
+
+// What the calls on dispatched rows share: topk, the row length, and the slots
+// (pos, and the binary32 values beside it) of at least one token.
+xred_status check_slots(uint64_t tokens, uint32_t topk, uint64_t hidden, uint64_t es)
+{
+    if (topk < 1 || topk > XRED_MAX_TOPK)
+        return fail(XRED_UNSUPPORTED, "topk = %u outside 1..%d", topk, XRED_MAX_TOPK);
+    if (hidden < 1 || hidden > (1u << 30) / es)
+        return fail(XRED_UNSUPPORTED, "hidden = %llu: rows of 1 element to 1 GiB are supported",
+                    (unsigned long long)hidden);
+    if (tokens > (uint64_t)INT64_MAX / (4 * XRED_MAX_TOPK))
+        return fail(XRED_INVALID_ARGUMENT, "tokens * topk overflows");
+    return XRED_SUCCESS;
+}
+
+xred_status check_words(const void *p, uint64_t tokens, uint64_t topk, const char *name, Matrix *out)
+{
+    return check_rows(xred_rows{(void *)p, topk}, tokens, topk, 4, name, out);
 }
 
 }  // namespace
@@ -253,6 +272,151 @@ XRED_API xred_status xred_route_grad(const xred_route_grad_args *args, void *hip
     TRY(check_apart(out, names, 1, in, 3, may));
     const hipError_t e = launch_route_grad(a, (hipStream_t)hip_stream);
     return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "route_grad launch");
+}
+
+XRED_API size_t xred_dispatch_plan_workspace(uint64_t slots, uint32_t experts)
+{
+    return experts > XRED_MAX_EXPERTS ? 0 : (size_t)dispatch_plan_bytes(slots, experts);
+}
+
+XRED_API xred_status xred_dispatch_plan(const xred_dispatch_plan_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_dispatch_plan_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_dispatch_plan tokens=%llu topk=%u experts=%u stream=%p",
+                     (unsigned long long)a.tokens, a.topk, a.experts, hip_stream);
+    if (a.experts < 1 || a.experts > XRED_MAX_EXPERTS)
+        return fail(XRED_UNSUPPORTED, "experts = %u outside 1..%d", a.experts, XRED_MAX_EXPERTS);
+    TRY(check_slots(a.tokens, a.topk, 1, 1));
+    const uint64_t n = a.tokens * a.topk;
+    if (n > INT32_MAX)
+        return fail(XRED_UNSUPPORTED, "%llu slots, at most 2^31 - 1 are supported",
+                    (unsigned long long)n);
+    Matrix in[1], out[5];
+    const char *names[5];
+    int nin = 0, nout = 0;
+    const int may[5] = {0, 0, 0, 0, 0};
+    auto output = [&](void *p, uint64_t words, const char *name) {
+        names[nout] = name;
+        return check_words(p, 1, words, name, &out[nout++]);
+    };
+    TRY(output(a.counts, a.experts, "counts"));
+    TRY(output(a.offsets, a.experts + 1, "offsets"));
+    if (n) {
+        TRY(check_words(a.ids, 1, n, "ids", &in[nin++]));
+        TRY(output(a.pos, n, "pos"));
+        if (a.slots) TRY(output(a.slots, n, "slots"));
+    }
+    const uint64_t need = dispatch_plan_bytes(n, a.experts);
+    if (a.workspace_bytes < need)
+        return fail(XRED_INVALID_ARGUMENT, "workspace of %llu bytes, %llu are needed",
+                    (unsigned long long)a.workspace_bytes, (unsigned long long)need);
+    if (need) {
+        TRY(check_buf(a.workspace, need, 16, "workspace", 0));
+        names[nout] = "workspace";
+        out[nout++] = Matrix{a.workspace, need, need, 1};
+    }
+    TRY(check_apart(out, names, nout, in, nin, may));
+    const hipError_t e = launch_dispatch_plan(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "dispatch_plan launch");
+}
+
+XRED_API xred_status xred_dispatch(const xred_dispatch_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_dispatch_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_dispatch tokens=%llu topk=%u hidden=%llu out_rows=%llu dtype=%d "
+                     "stream=%p", (unsigned long long)a.tokens, a.topk,
+                     (unsigned long long)a.hidden, (unsigned long long)a.out_rows, (int)a.dtype,
+                     hip_stream);
+    const uint64_t es = elem_size(a.dtype);
+    if (es == 0) return fail(XRED_INVALID_ARGUMENT, "unknown dtype %d", (int)a.dtype);
+    TRY(check_slots(a.tokens, a.topk, a.hidden, es));
+    if ((a.scale.data == nullptr) != (a.out_scale.data == nullptr) && a.tokens && a.out_rows)
+        return fail(XRED_INVALID_ARGUMENT, "scale and out_scale go together");
+    if (a.scale.data) TRY(check_slots(a.tokens, a.topk, a.scale_columns, 4));
+    if (a.tokens == 0 || a.out_rows == 0) return XRED_SUCCESS;
+    Matrix in[3], out[2];
+    const char *const names[2] = {"out", "out_scale"};
+    const int may[2] = {0, 0};
+    TRY(check_rows(a.x, a.tokens, a.hidden, es, "x", &in[0]));
+    TRY(check_words(a.pos, a.tokens, a.topk, "pos", &in[1]));
+    TRY(check_rows(a.out, a.out_rows, a.hidden, es, "out", &out[0]));
+    if (a.scale.data) {
+        TRY(check_rows(a.scale, a.tokens, a.scale_columns, 4, "scale", &in[2]));
+        TRY(check_rows(a.out_scale, a.out_rows, a.scale_columns, 4, "out_scale", &out[1]));
+    }
+    const int more = a.scale.data ? 1 : 0;
+    TRY(check_apart(out, names, 1 + more, in, 2 + more, may));
+    const hipError_t e = launch_dispatch(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "dispatch launch");
+}
+
+XRED_API xred_status xred_combine(const xred_combine_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_combine_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_combine tokens=%llu topk=%u hidden=%llu y_rows=%llu dtype=%d stream=%p",
+                     (unsigned long long)a.tokens, a.topk, (unsigned long long)a.hidden,
+                     (unsigned long long)a.y_rows, (int)a.dtype, hip_stream);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    const uint64_t es = elem_size(a.dtype);
+    TRY(check_slots(a.tokens, a.topk, a.hidden, es));
+    if (a.tokens == 0) return XRED_SUCCESS;
+    Matrix in[4], out[1];
+    const char *const names[1] = {"out"};
+    int nin = 0, may[1] = {0};
+    if (a.base.data) {
+        TRY(check_rows(a.base, a.tokens, a.hidden, es, "base", &in[nin++]));
+        may[0] = nin;
+    }
+    if (a.y_rows) TRY(check_rows(a.y, a.y_rows, a.hidden, es, "y", &in[nin++]));
+    TRY(check_words(a.pos, a.tokens, a.topk, "pos", &in[nin++]));
+    if (a.weights) TRY(check_words(a.weights, a.tokens, a.topk, "weights", &in[nin++]));
+    TRY(check_rows(a.out, a.tokens, a.hidden, es, "out", &out[0]));
+    TRY(check_apart(out, names, 1, in, nin, may));
+    const hipError_t e = launch_combine(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "combine launch");
+}
+
+XRED_API xred_status xred_combine_grad(const xred_combine_grad_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_combine_grad_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_combine_grad tokens=%llu topk=%u hidden=%llu y_rows=%llu dtype=%d "
+                     "stream=%p", (unsigned long long)a.tokens, a.topk,
+                     (unsigned long long)a.hidden, (unsigned long long)a.y_rows, (int)a.dtype,
+                     hip_stream);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    const uint64_t es = elem_size(a.dtype);
+    TRY(check_slots(a.tokens, a.topk, a.hidden, es));
+    if (a.tokens == 0) return XRED_SUCCESS;
+    Matrix in[4], out[2];
+    const char *names[2];
+    int nin = 0, nout = 0, may[2] = {0, 0};
+    if (a.y_rows) {
+        if (a.dweights) {
+            TRY(check_rows(a.y, a.y_rows, a.hidden, es, "y", &in[nin++]));
+            may[0] = nin;
+        }
+        names[nout] = "dy";
+        TRY(check_rows(a.dy, a.y_rows, a.hidden, es, "dy", &out[nout++]));
+    }
+    TRY(check_rows(a.dout, a.tokens, a.hidden, es, "dout", &in[nin++]));
+    TRY(check_words(a.pos, a.tokens, a.topk, "pos", &in[nin++]));
+    TRY(check_words(a.weights, a.tokens, a.topk, "weights", &in[nin++]));
+    if (a.dweights) {
+        names[nout] = "dweights";
+        TRY(check_words(a.dweights, a.tokens, a.topk, "dweights", &out[nout++]));
+    }
+    if (nout == 0) return XRED_SUCCESS;
+    TRY(check_apart(out, names, nout, in, nin, may));
+    const hipError_t e = launch_combine_grad(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "combine_grad launch");
 }
 
 }  // extern "C"

@@ -16,4 +16,11 @@ hipError_t launch_fold_norm_grad(const xred_fold_norm_grad_args &a, hipStream_t 
 hipError_t launch_route(const xred_route_args &a, hipStream_t stream);
 hipError_t launch_route_grad(const xred_route_grad_args &a, hipStream_t stream);
 
+// Bytes of workspace for n slots.
+uint64_t dispatch_plan_bytes(uint64_t n, uint32_t experts);
+hipError_t launch_dispatch_plan(const xred_dispatch_plan_args &a, hipStream_t stream);
+hipError_t launch_dispatch(const xred_dispatch_args &a, hipStream_t stream);
+hipError_t launch_combine(const xred_combine_args &a, hipStream_t stream);
+hipError_t launch_combine_grad(const xred_combine_grad_args &a, hipStream_t stream);
+
 }  // namespace xred

@@ -14,7 +14,8 @@ from __future__ import annotations
 import ctypes
 
 from . import _dtype_name, _ptr, _require, _stream
-from ._lib import (DTYPE, ELEM_SIZE, INVALID_ARGUMENT, ROUTE_RENORM, SCORE, FoldNormArgs,
+from ._lib import (DTYPE, ELEM_SIZE, INVALID_ARGUMENT, ROUTE_RENORM, SCORE, CombineArgs,
+                   CombineGradArgs, DispatchArgs, DispatchPlanArgs, FoldNormArgs,
                    FoldNormGradArgs, RouteArgs, RouteGradArgs, XredError, XredRows, check, load,
                    ptr_array)
 
@@ -196,3 +197,92 @@ def route_grad(logits, ids, dweights, dlogits, *, score: str = "softmax", renorm
         _slots(ids, tokens, topk, "ids", dev, ("i32",)),
         _slots(dweights, tokens, topk, "dweights", dev, ("f32",)), DTYPE[dt], _score(score), scale)
     check(load().xred_route_grad(ctypes.byref(a), _stream(logits, stream)))
+
+
+def _ints(t, n, what, device):
+    if t is not None and _dtype_name(t, None) != "i32":
+        _refuse(f"{what} is {t.dtype}, expected int32")
+    return _vector(t, n, 4, what, device)
+
+
+def dispatch_plan(ids, counts, offsets, pos, *, slots=None, workspace=None, stream=None) -> None:
+    """The order of routed rows by expert (xred_dispatch_plan), all int32.
+
+    ids: tokens x topk, -1 (or any id that is no expert) drops the slot; counts:
+    experts; offsets: experts + 1; pos: tokens x topk, each slot's row or -1;
+    slots (optional, tokens * topk): each row's slot.  workspace: a tensor to use
+    instead of one from torch's allocator."""
+    tokens, topk = _shape(ids, "ids")
+    experts, dev = counts.numel(), ids.device
+    L = load()
+    need = L.xred_dispatch_plan_workspace(tokens * topk, experts)
+    ws = _workspace(workspace, need, ids, stream) if need else None
+    a = DispatchPlanArgs(
+        tokens, experts, topk, _slots(ids, tokens, topk, "ids", dev, ("i32",)),
+        _ints(counts, experts, "counts", dev), _ints(offsets, experts + 1, "offsets", dev),
+        _slots(pos, tokens, topk, "pos", dev, ("i32",)),
+        _ints(slots, tokens * topk, "slots", dev), _ptr(ws),
+        ws.numel() * ws.element_size() if ws is not None else 0)
+    check(L.xred_dispatch_plan(ctypes.byref(a), _stream(ids, stream)))
+
+
+def dispatch(x, pos, out, *, scale=None, out_scale=None, stream=None) -> None:
+    """Rows to their places: out[pos[t][j]] = x[t] (xred_dispatch), any dtype; scale
+    (tokens x columns, fp32) travels along to out_scale."""
+    tokens, hidden = _shape(x, "x")
+    topk, rows = _shape(pos, "pos")[1], _shape(out, "out")[0]
+    dt, dev = _dtype_name(x, None), x.device
+    if out.dtype != x.dtype:
+        _refuse(f"out is {out.dtype}, x is {x.dtype}")
+    if (scale is None) != (out_scale is None):
+        _refuse("scale and out_scale go together")
+    for what, t in (("scale", scale), ("out_scale", out_scale)):
+        if t is not None and _dtype_name(t, None) != "f32":
+            _refuse(f"{what} is {t.dtype}, expected float32")
+    es = ELEM_SIZE[dt]
+    columns = _shape(scale, "scale")[1] if scale is not None else 0
+    a = DispatchArgs(
+        tokens, hidden, rows, columns, topk, DTYPE[dt], _matrix(x, tokens, hidden, es, "x", dev),
+        _matrix(out, rows, hidden, es, "out", dev), _matrix(scale, tokens, columns, 4, "scale", dev),
+        _matrix(out_scale, rows, columns, 4, "out_scale", dev),
+        _slots(pos, tokens, topk, "pos", dev, ("i32",)))
+    check(load().xred_dispatch(ctypes.byref(a), _stream(x, stream)))
+
+
+def combine(y, pos, out, *, weights=None, base=None, stream=None) -> None:
+    """The experts' rows back to their tokens (xred_combine):
+    out[t] = base[t] + sum over j of weights[t][j] * y[pos[t][j]], in order of j."""
+    rows, hidden = _shape(y, "y")
+    tokens, topk = _shape(pos, "pos")
+    dt, dev = _dtype_name(y, None), y.device
+    for what, t in (("out", out), ("base", base)):
+        if t is not None and t.dtype != y.dtype:
+            _refuse(f"{what} is {t.dtype}, y is {y.dtype}")
+    es = ELEM_SIZE[dt]
+    a = CombineArgs(
+        tokens, hidden, rows, topk, DTYPE[dt], _matrix(y, rows, hidden, es, "y", dev),
+        _matrix(base, tokens, hidden, es, "base", dev), _matrix(out, tokens, hidden, es, "out", dev),
+        _slots(pos, tokens, topk, "pos", dev, ("i32",)),
+        None if weights is None else _slots(weights, tokens, topk, "weights", dev, ("f32",)))
+    check(load().xred_combine(ctypes.byref(a), _stream(y, stream)))
+
+
+def combine_grad(dout, y, pos, weights, dy, dweights=None, *, stream=None) -> None:
+    """The gradient of combine (xred_combine_grad): dy, the experts' rows', and
+    dweights (fp32, tokens x topk); base's is dout itself."""
+    rows, hidden = _shape(dy, "dy")
+    tokens, topk = _shape(pos, "pos")
+    dt, dev = _dtype_name(dout, None), dout.device
+    if y is None and dweights is not None:
+        _refuse("dweights needs y")
+    for what, t in (("y", y), ("dy", dy)):
+        if t is not None and t.dtype != dout.dtype:
+            _refuse(f"{what} is {t.dtype}, dout is {dout.dtype}")
+    es = ELEM_SIZE[dt]
+    a = CombineGradArgs(
+        tokens, hidden, rows, topk, DTYPE[dt], _matrix(dout, tokens, hidden, es, "dout", dev),
+        _matrix(y, rows, hidden, es, "y", dev), _matrix(dy, rows, hidden, es, "dy", dev),
+        _slots(pos, tokens, topk, "pos", dev, ("i32",)),
+        _slots(weights, tokens, topk, "weights", dev, ("f32",)),
+        None if dweights is None else _slots(dweights, tokens, topk, "dweights", dev, ("f32",)))
+    check(load().xred_combine_grad(ctypes.byref(a), _stream(dout, stream)))
