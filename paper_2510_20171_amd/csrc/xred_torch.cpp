@@ -32,6 +32,16 @@ decltype(&xred_acc_cast) f_cast;
 decltype(&xred_batched_reduce) f_batched;
 decltype(&xred_ring_reduce) f_ring;
 decltype(&xred_allreduce_sim) f_sim;
+decltype(&xred_fold_norm) f_fold_norm;
+decltype(&xred_fold_norm_grad) f_fold_norm_grad;
+decltype(&xred_fold_norm_grad_workspace) f_fold_norm_grad_workspace;
+decltype(&xred_route) f_route;
+decltype(&xred_route_grad) f_route_grad;
+decltype(&xred_dispatch_plan) f_dispatch_plan;
+decltype(&xred_dispatch_plan_workspace) f_dispatch_plan_workspace;
+decltype(&xred_dispatch) f_dispatch;
+decltype(&xred_combine) f_combine;
+decltype(&xred_combine_grad) f_combine_grad;
 PyObject *current_raw_stream;
 
 // Raised to leave a call to the Python code.
@@ -346,6 +356,334 @@ PyObject *sim(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
+// ------------------------------------------------ around a reduced activation --
+// A matrix argument: a 2-D tensor of this shape, dtype and device whose rows are
+// contiguous; None where it may be absent.
+struct Matrix {
+    c10::Device dev;
+    int64_t rows, columns;
+    at::ScalarType type;
+
+    xred_rows operator()(PyObject *o) const { return (*this)(o, columns, type); }
+    xred_rows operator()(PyObject *o, int64_t n, at::ScalarType t) const
+    {
+        return o == Py_None ? xred_rows{nullptr, 0} : of(tensor(o), n, t);
+    }
+    xred_rows of(const at::Tensor &m, int64_t n, at::ScalarType t) const
+    {
+        if (!m.is_cuda() || m.device() != dev || m.scalar_type() != t || m.dim() != 2 ||
+            m.size(0) != rows || m.size(1) != n || (n > 1 && m.stride(1) != 1) ||
+            (rows > 1 && m.stride(0) < n))
+            throw Decline{};
+        return {m.data_ptr(), (uint64_t)(rows > 1 ? m.stride(0) : n)};
+    }
+};
+
+// The matrix that gives a call its shape, dtype (fp32, bf16 or fp16 unless
+// `any`) and device.
+Matrix lead(PyObject *o, xred_dtype *dtype, bool any = false)
+{
+    const at::Tensor &t = tensor(o);
+    if (!t.is_cuda() || t.dim() != 2) throw Decline{};
+    if (!any && t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16 &&
+        t.scalar_type() != at::kHalf)
+        throw Decline{};
+    *dtype = type_of(t, Py_None).code;
+    return {t.device(), t.size(0), t.size(1), t.scalar_type()};
+}
+
+// A contiguous tensor of n elements of one dtype, or None: nullptr.
+void *vector(PyObject *o, c10::Device dev, int64_t n, at::ScalarType type)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o);
+    if (t.scalar_type() != type) throw Decline{};
+    return data_of(t, dev, n, c10::elementSize(type));
+}
+
+// A contiguous tokens x topk tensor.
+void *slots(PyObject *o, c10::Device dev, int64_t tokens, int64_t topk, at::ScalarType type)
+{
+    const at::Tensor &t = tensor(o);
+    if (t.dim() != 2 || t.size(0) != tokens || t.size(1) != topk) throw Decline{};
+    return vector(o, dev, tokens * topk, type);
+}
+
+int64_t slots_per_token(PyObject *o)
+{
+    const at::Tensor &t = tensor(o);
+    if (t.dim() != 2) throw Decline{};
+    return t.size(1);
+}
+
+// Row weights in the call's dtype or fp32, or None.
+const void *row_weights(PyObject *o, const Matrix &m, xred_dtype dtype, xred_dtype *type)
+{
+    *type = dtype;
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o);
+    if (t.scalar_type() != m.type && t.scalar_type() != at::kFloat) throw Decline{};
+    *type = t.scalar_type() == m.type ? dtype : XRED_FLOAT32;
+    return data_of(t, m.dev, m.columns, t.element_size());
+}
+
+uint32_t u32_of(PyObject *o)
+{
+    if (!PyLong_CheckExact(o)) throw Decline{};
+    int over = 0;
+    const long x = PyLong_AsLongAndOverflow(o, &over);
+    if (over || x < 0 || x > INT32_MAX) throw Decline{};
+    return (uint32_t)x;
+}
+
+float float_of(PyObject *o)
+{
+    if (PyFloat_CheckExact(o)) return (float)PyFloat_AS_DOUBLE(o);
+    if (!PyLong_CheckExact(o)) throw Decline{};
+    const double x = PyLong_AsDouble(o);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Decline{};
+    }
+    return (float)x;
+}
+
+xred_score score_of(PyObject *o)
+{
+    if (text_is(o, "softmax")) return XRED_SCORE_SOFTMAX;
+    if (text_is(o, "sigmoid")) return XRED_SCORE_SIGMOID;
+    throw Decline{};
+}
+
+// The caller's workspace; a call that needs one but was given none is left to
+// the Python code, which allocates it.
+void *workspace_of(PyObject *o, c10::Device dev, uint64_t need, uint64_t *bytes)
+{
+    *bytes = 0;
+    if (need == 0) return nullptr;
+    const at::Tensor &t = tensor(o);
+    if (!t.is_cuda() || t.device() != dev || !t.is_contiguous()) throw Decline{};
+    *bytes = (uint64_t)t.numel() * t.element_size();
+    return t.data_ptr();
+}
+
+// fold_norm(srcs, out, residual, weight, sum, out8, scale, rstd, group, eps, stream)
+PyObject *fold_norm(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 11, [&] {
+        if (!PyList_CheckExact(a[0]) && !PyTuple_CheckExact(a[0])) throw Decline{};
+        const Py_ssize_t nsrc = PySequence_Fast_GET_SIZE(a[0]);
+        if (nsrc < 1 || nsrc > XRED_MAX_SRC) throw Decline{};
+        PyObject **src = PySequence_Fast_ITEMS(a[0]);
+        xred_fold_norm_args n{};
+        const Matrix m = lead(src[0], &n.dtype);
+        const void *ptrs[XRED_MAX_SRC];
+        n.srcs = ptrs;
+        n.nsrc = (uint32_t)nsrc;
+        for (Py_ssize_t i = 0; i < nsrc; ++i) {
+            const xred_rows s = m(src[i]);
+            if (i != 0 && s.stride != n.src_stride) throw Decline{};
+            n.src_stride = s.stride;
+            ptrs[i] = s.data;
+        }
+        n.group = u32_of(a[8]);
+        n.rows = (uint64_t)m.rows;
+        n.hidden = (uint64_t)m.columns;
+        n.residual = m(a[2]);
+        n.sum = m(a[4]);
+        n.out = m(a[1]);
+        if (a[5] != Py_None) {
+            const at::ScalarType t = tensor(a[5]).scalar_type();
+            if (t != at::kFloat8_e4m3fn && t != at::kByte) throw Decline{};
+            n.out8 = m(a[5], m.columns, t);
+        }
+        n.scale = m(a[6], n.group ? (m.columns + n.group - 1) / n.group : 1, at::kFloat);
+        n.weight = row_weights(a[3], m, n.dtype, &n.weight_dtype);
+        n.rstd = (float *)vector(a[7], m.dev, m.rows, at::kFloat);
+        n.eps = float_of(a[9]);
+        void *stream = stream_of(a[10], m.dev);
+        return unlocked([&] { return f_fold_norm(&n, stream); });
+    });
+}
+
+// fold_norm_grad(dout, sum, rstd, dx, weight, dsum, dweight, workspace, stream)
+PyObject *fold_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 9, [&] {
+        xred_fold_norm_grad_args n{};
+        const Matrix m = lead(a[1], &n.dtype);
+        n.rows = (uint64_t)m.rows;
+        n.hidden = (uint64_t)m.columns;
+        n.dout = m(a[0]);
+        n.sum = m(a[1]);
+        n.dsum = m(a[5]);
+        n.dx = m(a[3]);
+        n.weight = row_weights(a[4], m, n.dtype, &n.weight_dtype);
+        n.rstd = (const float *)vector(a[2], m.dev, m.rows, at::kFloat);
+        n.dweight = (float *)vector(a[6], m.dev, m.columns, at::kFloat);
+        const uint64_t need = n.dweight ? f_fold_norm_grad_workspace(n.rows, n.hidden) : 0;
+        n.workspace = workspace_of(a[7], m.dev, need, &n.workspace_bytes);
+        void *stream = stream_of(a[8], m.dev);
+        return unlocked([&] { return f_fold_norm_grad(&n, stream); });
+    });
+}
+
+// route(logits, ids, weights, score, bias, groups, group_topk, group_score, renorm, scale, stream)
+PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 11, [&] {
+        xred_route_args n{};
+        const Matrix m = lead(a[0], &n.dtype);
+        const int64_t k = slots_per_token(a[1]);
+        if (m.columns > XRED_MAX_EXPERTS || k > XRED_MAX_TOPK) throw Decline{};
+        n.tokens = (uint64_t)m.rows;
+        n.experts = (uint32_t)m.columns;
+        n.topk = (uint32_t)k;
+        n.groups = u32_of(a[5]);
+        n.group_topk = u32_of(a[6]);
+        n.group_score = u32_of(a[7]);
+        n.flags = a[8] == Py_True ? XRED_ROUTE_RENORM : a[8] == Py_False ? 0u : throw Decline{};
+        n.logits = m(a[0]);
+        n.bias = (const float *)vector(a[4], m.dev, m.columns, at::kFloat);
+        n.ids = (int32_t *)slots(a[1], m.dev, m.rows, k, at::kInt);
+        n.weights = (float *)slots(a[2], m.dev, m.rows, k, at::kFloat);
+        n.score = score_of(a[3]);
+        n.scale = float_of(a[9]);
+        void *stream = stream_of(a[10], m.dev);
+        return unlocked([&] { return f_route(&n, stream); });
+    });
+}
+
+// route_grad(logits, ids, dweights, dlogits, score, renorm, scale, stream)
+PyObject *route_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 8, [&] {
+        xred_route_grad_args n{};
+        const Matrix m = lead(a[0], &n.dtype);
+        const int64_t k = slots_per_token(a[1]);
+        if (m.columns > XRED_MAX_EXPERTS || k > XRED_MAX_TOPK) throw Decline{};
+        n.tokens = (uint64_t)m.rows;
+        n.experts = (uint32_t)m.columns;
+        n.topk = (uint32_t)k;
+        n.flags = a[5] == Py_True ? XRED_ROUTE_RENORM : a[5] == Py_False ? 0u : throw Decline{};
+        n.logits = m(a[0]);
+        n.dlogits = m(a[3]);
+        n.ids = (const int32_t *)slots(a[1], m.dev, m.rows, k, at::kInt);
+        n.dweights = (const float *)slots(a[2], m.dev, m.rows, k, at::kFloat);
+        n.score = score_of(a[4]);
+        n.scale = float_of(a[6]);
+        void *stream = stream_of(a[7], m.dev);
+        return unlocked([&] { return f_route_grad(&n, stream); });
+    });
+}
+
+// dispatch_plan(ids, counts, offsets, pos, slots, workspace, stream)
+PyObject *dispatch_plan(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 7, [&] {
+        const at::Tensor &ids = tensor(a[0]), &counts = tensor(a[1]);
+        if (!ids.is_cuda() || ids.dim() != 2) throw Decline{};
+        const c10::Device dev = ids.device();
+        const int64_t tokens = ids.size(0), k = ids.size(1), experts = counts.numel();
+        if (experts < 1 || experts > XRED_MAX_EXPERTS || k < 1 || k > XRED_MAX_TOPK) throw Decline{};
+        xred_dispatch_plan_args n{};
+        n.tokens = (uint64_t)tokens;
+        n.experts = (uint32_t)experts;
+        n.topk = (uint32_t)k;
+        n.ids = (const int32_t *)slots(a[0], dev, tokens, k, at::kInt);
+        n.counts = (int32_t *)vector(a[1], dev, experts, at::kInt);
+        n.offsets = (int32_t *)vector(a[2], dev, experts + 1, at::kInt);
+        n.pos = (int32_t *)slots(a[3], dev, tokens, k, at::kInt);
+        n.slots = (int32_t *)vector(a[4], dev, tokens * k, at::kInt);
+        n.workspace = workspace_of(a[5], dev,
+                                   f_dispatch_plan_workspace((uint64_t)(tokens * k), n.experts),
+                                   &n.workspace_bytes);
+        void *stream = stream_of(a[6], dev);
+        return unlocked([&] { return f_dispatch_plan(&n, stream); });
+    });
+}
+
+// dispatch(x, pos, out, scale, out_scale, stream)
+PyObject *dispatch(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 6, [&] {
+        xred_dispatch_args n{};
+        const Matrix m = lead(a[0], &n.dtype, true);
+        const int64_t k = slots_per_token(a[1]);
+        if (k < 1 || k > XRED_MAX_TOPK || (a[3] == Py_None) != (a[4] == Py_None)) throw Decline{};
+        const at::Tensor &out = tensor(a[2]);
+        if (out.dim() != 2) throw Decline{};
+        const Matrix to{m.dev, out.size(0), m.columns, m.type};
+        n.tokens = (uint64_t)m.rows;
+        n.hidden = (uint64_t)m.columns;
+        n.out_rows = (uint64_t)to.rows;
+        n.topk = (uint32_t)k;
+        n.x = m(a[0]);
+        n.out = to(a[2]);
+        if (a[3] != Py_None) {
+            const int64_t columns = slots_per_token(a[3]);
+            n.scale_columns = (uint64_t)columns;
+            n.scale = m(a[3], columns, at::kFloat);
+            n.out_scale = to(a[4], columns, at::kFloat);
+        }
+        n.pos = (const int32_t *)slots(a[1], m.dev, m.rows, k, at::kInt);
+        void *stream = stream_of(a[5], m.dev);
+        return unlocked([&] { return f_dispatch(&n, stream); });
+    });
+}
+
+// combine(y, pos, out, weights, base, stream)
+PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 6, [&] {
+        xred_combine_args n{};
+        const Matrix m = lead(a[0], &n.dtype);
+        const at::Tensor &pos = tensor(a[1]);
+        const int64_t k = slots_per_token(a[1]);
+        if (k < 1 || k > XRED_MAX_TOPK) throw Decline{};
+        const Matrix to{m.dev, pos.size(0), m.columns, m.type};
+        n.tokens = (uint64_t)to.rows;
+        n.hidden = (uint64_t)m.columns;
+        n.y_rows = (uint64_t)m.rows;
+        n.topk = (uint32_t)k;
+        n.y = m(a[0]);
+        n.base = to(a[4]);
+        if (a[2] == Py_None) throw Decline{};
+        n.out = to(a[2]);
+        n.pos = (const int32_t *)slots(a[1], m.dev, to.rows, k, at::kInt);
+        if (a[3] != Py_None)
+            n.weights = (const float *)slots(a[3], m.dev, to.rows, k, at::kFloat);
+        void *stream = stream_of(a[5], m.dev);
+        return unlocked([&] { return f_combine(&n, stream); });
+    });
+}
+
+// combine_grad(dout, y, pos, weights, dy, dweights, stream)
+PyObject *combine_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 7, [&] {
+        xred_combine_grad_args n{};
+        const Matrix m = lead(a[0], &n.dtype);
+        const at::Tensor &dy = tensor(a[4]);
+        const int64_t k = slots_per_token(a[2]);
+        if (k < 1 || k > XRED_MAX_TOPK || dy.dim() != 2) throw Decline{};
+        if (a[1] == Py_None && a[5] != Py_None) throw Decline{};
+        const Matrix to{m.dev, dy.size(0), m.columns, m.type};
+        n.tokens = (uint64_t)m.rows;
+        n.hidden = (uint64_t)m.columns;
+        n.y_rows = (uint64_t)to.rows;
+        n.topk = (uint32_t)k;
+        n.dout = m(a[0]);
+        n.y = to(a[1]);
+        n.dy = to(a[4]);
+        n.pos = (const int32_t *)slots(a[2], m.dev, m.rows, k, at::kInt);
+        n.weights = (const float *)slots(a[3], m.dev, m.rows, k, at::kFloat);
+        if (a[5] != Py_None) n.dweights = (float *)slots(a[5], m.dev, m.rows, k, at::kFloat);
+        void *stream = stream_of(a[6], m.dev);
+        return unlocked([&] { return f_combine_grad(&n, stream); });
+    });
+}
+
 // bind(current_raw_stream, {name: address}): once, by the loader.
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -363,6 +701,13 @@ PyObject *bind(PyObject *, PyObject *args)
     if (!take("xred_reduce_scatter_local", f_scatter) || !take("xred_reduce_copy_step", f_step) ||
         !take("xred_acc_cast", f_cast) || !take("xred_batched_reduce", f_batched) ||
         !take("xred_ring_reduce", f_ring) || !take("xred_allreduce_sim", f_sim) ||
+        !take("xred_fold_norm", f_fold_norm) || !take("xred_fold_norm_grad", f_fold_norm_grad) ||
+        !take("xred_fold_norm_grad_workspace", f_fold_norm_grad_workspace) ||
+        !take("xred_route", f_route) || !take("xred_route_grad", f_route_grad) ||
+        !take("xred_dispatch_plan", f_dispatch_plan) ||
+        !take("xred_dispatch_plan_workspace", f_dispatch_plan_workspace) ||
+        !take("xred_dispatch", f_dispatch) || !take("xred_combine", f_combine) ||
+        !take("xred_combine_grad", f_combine_grad) ||
         !take("xred_allreduce_local", all))
         return nullptr;
     Py_INCREF(get);
@@ -380,6 +725,14 @@ PyMethodDef methods[] = {
     {"batched", (PyCFunction)(void *)batched, METH_FASTCALL, nullptr},
     {"ring", (PyCFunction)(void *)ring, METH_FASTCALL, nullptr},
     {"sim", (PyCFunction)(void *)sim, METH_FASTCALL, nullptr},
+    {"fold_norm", (PyCFunction)(void *)fold_norm, METH_FASTCALL, nullptr},
+    {"fold_norm_grad", (PyCFunction)(void *)fold_norm_grad, METH_FASTCALL, nullptr},
+    {"route", (PyCFunction)(void *)route, METH_FASTCALL, nullptr},
+    {"route_grad", (PyCFunction)(void *)route_grad, METH_FASTCALL, nullptr},
+    {"dispatch_plan", (PyCFunction)(void *)dispatch_plan, METH_FASTCALL, nullptr},
+    {"dispatch", (PyCFunction)(void *)dispatch, METH_FASTCALL, nullptr},
+    {"combine", (PyCFunction)(void *)combine, METH_FASTCALL, nullptr},
+    {"combine_grad", (PyCFunction)(void *)combine_grad, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_xred_torch",

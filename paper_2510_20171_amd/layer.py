@@ -17,7 +17,7 @@ from . import _dtype_name, _ptr, _require, _stream
 from ._lib import (DTYPE, ELEM_SIZE, INVALID_ARGUMENT, ROUTE_RENORM, SCORE, CombineArgs,
                    CombineGradArgs, DispatchArgs, DispatchPlanArgs, FoldNormArgs,
                    FoldNormGradArgs, RouteArgs, RouteGradArgs, XredError, XredRows, check, load,
-                   ptr_array)
+                   native, ptr_array)
 
 
 def _refuse(text):
@@ -82,19 +82,25 @@ def _weight(t, dtype, n, device):
     return _vector(t, n, ELEM_SIZE[name], "weight", device), DTYPE[name]
 
 
-def _workspace(t, nbytes, like, stream):
-    """The caller's workspace, or one from torch's allocator."""
+def _workspace(nbytes, like, stream):
+    """A workspace from torch's allocator, which knows it by the stream of the call."""
     import torch
-    if t is None:
-        t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-        if stream is not None:   # else it belongs to the stream the call runs on
-            if not isinstance(stream, torch.cuda.Stream):
-                handle = int(getattr(stream, "cuda_stream", stream))
-                stream = torch.cuda.ExternalStream(handle, device=like.device)
-            t.record_stream(stream)
-    elif not t.is_cuda or t.device != like.device or not t.is_contiguous():
-        _refuse("workspace is not a contiguous tensor of the call's device")
+    t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    if stream is not None:   # else it belongs to the stream the call runs on
+        if not isinstance(stream, torch.cuda.Stream):
+            handle = int(getattr(stream, "cuda_stream", stream))
+            stream = torch.cuda.ExternalStream(handle, device=like.device)
+        t.record_stream(stream)
     return t
+
+
+def _given(t, device):
+    """(pointer, bytes) of a workspace tensor, or of none."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.device != device or not t.is_contiguous():
+        _refuse(f"workspace is not a contiguous tensor on {device}")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def fold_norm(srcs, out=None, *, residual=None, weight=None, sum=None, out8=None, scale=None,
@@ -105,6 +111,10 @@ def fold_norm(srcs, out=None, *, residual=None, weight=None, sum=None, out8=None
     out8 the same in e4m3 with a scale for each row (group = 0) or group of
     elements; rstd the rows' 1 / sqrt(mean(h^2) + eps).  All but one of out and
     out8 is optional."""
+    st = native().fold_norm(srcs, out, residual, weight, sum, out8, scale, rstd, group, eps,
+                            stream)
+    if st is not None:   # plain tensors; anything else is checked below
+        return check(st)
     if len(srcs) < 1:
         _refuse("no sources")
     rows, hidden = _shape(srcs[0], "srcs[0]")
@@ -140,24 +150,25 @@ def fold_norm_grad(dout, sum, rstd, dx, *, weight=None, dsum=None, dweight=None,
     the residual and of every source, and dweight (fp32).  dsum: the gradient
     that reaches fold_norm's sum; workspace: a tensor to use for dweight's
     partial sums instead of one from torch's allocator."""
+    if dweight is not None and workspace is None:
+        workspace = _workspace(load().xred_fold_norm_grad_workspace(*_shape(sum, "sum")), sum,
+                               stream)
+    st = native().fold_norm_grad(dout, sum, rstd, dx, weight, dsum, dweight, workspace, stream)
+    if st is not None:   # plain tensors; anything else is checked below
+        return check(st)
     rows, hidden = _shape(sum, "sum")
     dt, dev = _dtype_name(sum, None), sum.device
     es = ELEM_SIZE[dt]
     for what, t in (("dout", dout), ("dsum", dsum), ("dx", dx)):
         if t is not None and t.dtype != sum.dtype:
             _refuse(f"{what} is {t.dtype}, sum is {sum.dtype}")
-    L = load()
-    ws = None
-    if dweight is not None:
-        ws = _workspace(workspace, L.xred_fold_norm_grad_workspace(rows, hidden), sum, stream)
     w, wt = _weight(weight, dt, hidden, dev)
     a = FoldNormGradArgs(
         rows, hidden, _matrix(dout, rows, hidden, es, "dout", dev),
         _matrix(sum, rows, hidden, es, "sum", dev), _matrix(dsum, rows, hidden, es, "dsum", dev),
         _matrix(dx, rows, hidden, es, "dx", dev), w, _floats(rstd, rows, "rstd", dev),
-        _floats(dweight, hidden, "dweight", dev), _ptr(ws),
-        ws.numel() * ws.element_size() if ws is not None else 0, DTYPE[dt], wt)
-    check(L.xred_fold_norm_grad(ctypes.byref(a), _stream(sum, stream)))
+        _floats(dweight, hidden, "dweight", dev), *_given(workspace, dev), DTYPE[dt], wt)
+    check(load().xred_fold_norm_grad(ctypes.byref(a), _stream(sum, stream)))
 
 
 def route(logits, ids, weights, *, score: str = "softmax", bias=None, groups: int = 1,
@@ -170,6 +181,10 @@ def route(logits, ids, weights, *, score: str = "softmax", bias=None, groups: in
     "sigmoid"; bias (fp32, one an expert) steers the choice only; with groups > 1
     the group_topk best groups of experts are chosen from, ranked by their best
     key (group_score = 1) or their best two."""
+    st = native().route(logits, ids, weights, score, bias, groups, group_topk, group_score,
+                        renorm, scale, stream)
+    if st is not None:   # plain tensors; anything else is checked below
+        return check(st)
     tokens, experts = _shape(logits, "logits")
     topk = _shape(ids, "ids")[1]
     dt, dev = _dtype_name(logits, None), logits.device
@@ -184,6 +199,9 @@ def route(logits, ids, weights, *, score: str = "softmax", bias=None, groups: in
 def route_grad(logits, ids, dweights, dlogits, *, score: str = "softmax", renorm: bool = True,
                scale: float = 1.0, stream=None) -> None:
     """The gradient of route's weights with respect to the logits (xred_route_grad)."""
+    st = native().route_grad(logits, ids, dweights, dlogits, score, renorm, scale, stream)
+    if st is not None:   # plain tensors; anything else is checked below
+        return check(st)
     tokens, experts = _shape(logits, "logits")
     topk = _shape(ids, "ids")[1]
     dt, dev = _dtype_name(logits, None), logits.device
@@ -212,23 +230,29 @@ def dispatch_plan(ids, counts, offsets, pos, *, slots=None, workspace=None, stre
     experts; offsets: experts + 1; pos: tokens x topk, each slot's row or -1;
     slots (optional, tokens * topk): each row's slot.  workspace: a tensor to use
     instead of one from torch's allocator."""
+    if workspace is None:
+        tokens, topk = _shape(ids, "ids")
+        need = load().xred_dispatch_plan_workspace(tokens * topk, counts.numel())
+        workspace = _workspace(need, ids, stream) if need else None
+    st = native().dispatch_plan(ids, counts, offsets, pos, slots, workspace, stream)
+    if st is not None:   # plain tensors; anything else is checked below
+        return check(st)
     tokens, topk = _shape(ids, "ids")
     experts, dev = counts.numel(), ids.device
-    L = load()
-    need = L.xred_dispatch_plan_workspace(tokens * topk, experts)
-    ws = _workspace(workspace, need, ids, stream) if need else None
     a = DispatchPlanArgs(
         tokens, experts, topk, _slots(ids, tokens, topk, "ids", dev, ("i32",)),
         _ints(counts, experts, "counts", dev), _ints(offsets, experts + 1, "offsets", dev),
         _slots(pos, tokens, topk, "pos", dev, ("i32",)),
-        _ints(slots, tokens * topk, "slots", dev), _ptr(ws),
-        ws.numel() * ws.element_size() if ws is not None else 0)
-    check(L.xred_dispatch_plan(ctypes.byref(a), _stream(ids, stream)))
+        _ints(slots, tokens * topk, "slots", dev), *_given(workspace, dev))
+    check(load().xred_dispatch_plan(ctypes.byref(a), _stream(ids, stream)))
 
 
 def dispatch(x, pos, out, *, scale=None, out_scale=None, stream=None) -> None:
     """Rows to their places: out[pos[t][j]] = x[t] (xred_dispatch), any dtype; scale
     (tokens x columns, fp32) travels along to out_scale."""
+    st = native().dispatch(x, pos, out, scale, out_scale, stream)
+    if st is not None:   # plain tensors; anything else is checked below
+        return check(st)
     tokens, hidden = _shape(x, "x")
     topk, rows = _shape(pos, "pos")[1], _shape(out, "out")[0]
     dt, dev = _dtype_name(x, None), x.device
@@ -252,6 +276,9 @@ def dispatch(x, pos, out, *, scale=None, out_scale=None, stream=None) -> None:
 def combine(y, pos, out, *, weights=None, base=None, stream=None) -> None:
     """The experts' rows back to their tokens (xred_combine):
     out[t] = base[t] + sum over j of weights[t][j] * y[pos[t][j]], in order of j."""
+    st = native().combine(y, pos, out, weights, base, stream)
+    if st is not None:   # plain tensors; anything else is checked below
+        return check(st)
     rows, hidden = _shape(y, "y")
     tokens, topk = _shape(pos, "pos")
     dt, dev = _dtype_name(y, None), y.device
@@ -270,6 +297,9 @@ def combine(y, pos, out, *, weights=None, base=None, stream=None) -> None:
 def combine_grad(dout, y, pos, weights, dy, dweights=None, *, stream=None) -> None:
     """The gradient of combine (xred_combine_grad): dy, the experts' rows', and
     dweights (fp32, tokens x topk); base's is dout itself."""
+    st = native().combine_grad(dout, y, pos, weights, dy, dweights, stream)
+    if st is not None:   # plain tensors; anything else is checked below
+        return check(st)
     rows, hidden = _shape(dy, "dy")
     tokens, topk = _shape(pos, "pos")
     dt, dev = _dtype_name(dout, None), dout.device
