@@ -302,7 +302,7 @@ __global__ __launch_bounds__(64 * kItemWaves) void combine_kernel(CombineParams 
     const uint32_t lane = threadIdx.x % 64;
     for (Item it(p.items); it.token < p.items.tokens; it.next(p.items)) {
         const uint32_t piece = it.tile * 64 + lane, c = piece_count(piece, p.hidden);
-        const uint32_t off = piece * 8 * T::kSize, whole = c == 8 ? off : 0;
+        const uint32_t from = piece_from(piece, c, p.hidden) * T::kSize;
         const int32_t *pos = p.pos + it.token * p.topk;
         const float *weights = p.weights ? p.weights + it.token * p.topk : nullptr;
         const char *base = p.base ? p.base + it.token * p.base_stride : nullptr;
@@ -318,52 +318,39 @@ __global__ __launch_bounds__(64 * kItemWaves) void combine_kernel(CombineParams 
             for (int i = 0; i < 8; ++i) acc[i] += weighted ? w * x[i] : x[i];
         };
         clear();
-        if (p.hidden >= 8) {
-            Piece<T> b;
-            if (base) b = load_piece<T>(base, whole);
-            for (uint32_t j0 = 0; j0 < p.topk; j0 += kCombineSlots) {
-                Piece<T> in[kCombineSlots];
-                bool on[kCombineSlots];
+        Piece<T> b;
+        if (base && p.hidden >= 8) b = load_piece<T>(base, from);
+        for (uint32_t j0 = 0; j0 < p.topk; j0 += kCombineSlots) {
+            Piece<T> in[kCombineSlots];
+            bool on[kCombineSlots];
+            const char *row[kCombineSlots];
 #pragma unroll
-                for (int g = 0; g < kCombineSlots; ++g) {
-                    const int32_t from = j0 + g < p.topk ? sload(pos + j0 + g) : -1;
-                    on[g] = from >= 0 && (uint64_t)from < p.y_rows;
-                    if (on[g]) in[g] = load_piece<T>(p.y + (uint64_t)from * p.y_stride, whole);
-                }
-                if (j0 == 0 && base) {
-                    float x[8];
-                    up_piece<T>(b, x);
-                    fold(x, 1.0f, false);
-                }
-#pragma unroll
-                for (int g = 0; g < kCombineSlots; ++g)
-                    if (on[g]) {
-                        any = true;
-                        float x[8];
-                        up_piece<T>(in[g], x);
-                        fold(x, weights ? sload(weights + j0 + g) : 1.0f, weights != nullptr);
-                    }
+            for (int g = 0; g < kCombineSlots; ++g) {
+                const int32_t at = j0 + g < p.topk ? sload(pos + j0 + g) : -1;
+                on[g] = at >= 0 && (uint64_t)at < p.y_rows;
+                row[g] = p.y + (on[g] ? (uint64_t)at * p.y_stride : 0);
+                if (on[g] && p.hidden >= 8) in[g] = load_piece<T>(row[g], from);
             }
-        }
-        if (c != 0 && c != 8) {   // the row's end, by one lane
-            clear();
             float x[8];
-            if (base) {
-                up_short<T>(base, off, c, x);
+            if (j0 == 0 && base) {
+                if (p.hidden >= 8) up_piece<T>(b, x);
+                else up_short<T>(base, c, x);
                 fold(x, 1.0f, false);
             }
-            for (uint32_t j = 0; j < p.topk; ++j) {
-                const int32_t from = pos[j];
-                if (from < 0 || (uint64_t)from >= p.y_rows) continue;
-                any = true;
-                up_short<T>(p.y + (uint64_t)from * p.y_stride, off, c, x);
-                fold(x, weights ? weights[j] : 1.0f, weights != nullptr);
-            }
+#pragma unroll
+            for (int g = 0; g < kCombineSlots; ++g)
+                if (on[g]) {
+                    any = true;
+                    if (p.hidden >= 8) up_piece<T>(in[g], x);
+                    else up_short<T>(row[g], c, x);
+                    fold(x, weights ? sload(weights + j0 + g) : 1.0f, weights != nullptr);
+                }
         }
         if (!any)
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
-        store_piece<T>(p.out + it.token * p.out_stride, off, c, acc);
+        if (p.hidden >= 8) settle(acc, c, p.hidden);
+        store_piece<T>(p.out + it.token * p.out_stride, piece * 8 * T::kSize, c, acc);
     }
 }
 
@@ -408,44 +395,43 @@ __global__ __launch_bounds__(TPR *RPB) void combine_grad_kernel(CombineGradParam
                 dot[g] = 0.0f;
             }
             for (uint32_t i = tid; i < pieces; i += TPR) {
-                const uint32_t c = piece_count(i, p.hidden), off = i * 8 * T::kSize;
-                float d[8];
-                if (c == 8) {
-                    Piece<T> in[kCombineSlots];
-                    const Piece<T> a = load_piece<T, true>(dout, off);
+                const uint32_t c = piece_count(i, p.hidden);
+                const uint32_t from = piece_from(i, c, p.hidden) * T::kSize;
+                const bool whole = p.hidden >= 8;
+                Piece<T> a, in[kCombineSlots];
+                if (whole) {
+                    a = load_piece<T, true>(dout, from);
                     if (p.dweights)
 #pragma unroll
                         for (int g = 0; g < kCombineSlots; ++g)
-                            if (on[g]) in[g] = load_piece<T>(p.y + row[g] * p.y_stride, off);
-                    up_piece<T>(a, d);
-                    if (p.dweights)
-#pragma unroll
-                        for (int g = 0; g < kCombineSlots; ++g)
-                            if (on[g]) {
-                                float x[8];
-                                up_piece<T>(in[g], x);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) dot[g] += d[e] * x[e];
-                            }
-                } else {
-                    up_short<T>(dout, off, c, d);
-                    if (p.dweights)
-#pragma unroll
-                        for (int g = 0; g < kCombineSlots; ++g)
-                            if (on[g]) {
-                                float x[8];
-                                up_short<T>(p.y + row[g] * p.y_stride, off, c, x);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) dot[g] += d[e] * x[e];
-                            }
+                            if (on[g]) in[g] = load_piece<T>(p.y + row[g] * p.y_stride, from);
                 }
+                float d[8], x[8];
+                if (whole) {
+                    up_piece<T>(a, d);
+                    settle(d, c, p.hidden);
+                } else {
+                    up_short<T>(dout, c, d);
+                }
+                if (p.dweights)
+#pragma unroll
+                    for (int g = 0; g < kCombineSlots; ++g)
+                        if (on[g]) {
+                            if (whole) {
+                                up_piece<T>(in[g], x);
+                                settle(x, c, p.hidden);
+                            } else {
+                                up_short<T>(p.y + row[g] * p.y_stride, c, x);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) dot[g] = __builtin_fmaf(d[e], x[e], dot[g]);
+                        }
 #pragma unroll
                 for (int g = 0; g < kCombineSlots; ++g)
                     if (on[g]) {
-                        float x[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = w[g] * d[e];
-                        store_piece<T>(p.dy + row[g] * p.dy_stride, off, c, x);
+                        store_piece<T>(p.dy + row[g] * p.dy_stride, i * 8 * T::kSize, c, x);
                     }
             }
             if (!p.dweights) continue;

@@ -13,6 +13,7 @@ namespace {
 // Sources folded into registers, at most this many 16-byte loads of them in
 // flight a lane (with the residual's and the weight's).
 constexpr int kInFlight = 8;
+constexpr int kRowsPerWg = 4;   // where a wave holds a row
 
 // The source pointers, by value (a type of its own: an expression of the header's
 // unnamed enum in a kernel's parameters gives it other names on host and device).
@@ -30,47 +31,55 @@ struct NormParams {
     uint64_t src_stride, residual_stride, sum_stride, out_stride;   // bytes
     uint64_t out8_stride, scale_stride;                             // elements
     uint32_t hidden, nsrc, group, wide_weight;
-    float eps;
+    float eps, inv_hidden;
 };
 
-// weight's piece (c elements at element e) as binary32; ones without a weight.
+// weight's piece i (c elements of it) as binary32; ones without a weight.
 template <class T>
-__device__ __forceinline__ void weight_piece(const char *w, bool wide, uint32_t e, uint32_t c,
-                                             float (&a)[8])
+__device__ __forceinline__ void weight_piece(const char *w, bool wide, uint32_t i, uint32_t c,
+                                             uint32_t n, float (&a)[8])
 {
     if (w == nullptr) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) a[j] = 1.0f;
-    } else if (wide) {
-        if (c == 8) up_piece<TF32>(load_piece<TF32, true>(w, 4 * e), a);
-        else up_short<TF32>(w, 4 * e, c, a);
+    } else if (n < 8) {
+        if (wide) up_short<TF32>(w, c, a);
+        else up_short<T>(w, c, a);
     } else {
-        if (c == 8) up_piece<T>(load_piece<T, true>(w, T::kSize * e), a);
-        else up_short<T>(w, T::kSize * e, c, a);
+        const uint32_t from = piece_from(i, c, n);
+        if (wide) up_piece<TF32>(load_piece<TF32, true>(w, 4 * from), a);
+        else up_piece<T>(load_piece<T, true>(w, T::kSize * from), a);
+        settle(a, c, n);
     }
 }
 
-// Sum and maximum over the TPR threads of a row.  WAVES > 1: red holds 2 * WAVES
-// floats, and a barrier has to come between two uses of it.
-template <int WAVES>
-__device__ __forceinline__ void row_reduce(float &s, float &m, float *red)
+// Rows of four pieces a thread leave no registers for the loads of one piece to
+// run ahead into the work on another.
+template <int V>
+__device__ __forceinline__ void narrow()
+{
+    if constexpr (V >= 4) __builtin_amdgcn_sched_barrier(0);
+}
+
+// Sum, and with MAX a maximum of magnitudes, over the waves of a row.  WG: the
+// workgroup's waves share the row; red then holds 2 * kMostWaves floats, and a
+// barrier has to come between two uses of it.
+constexpr int kMostWaves = 16;
+template <bool WG>
+__device__ __forceinline__ void row_reduce(float &s, float &m, bool max, float *red)
 {
     s = lanes_sum<64>(s);
-    m = lanes_max<64>(m);
-    if constexpr (WAVES > 1) {
-        const int wave = threadIdx.x / 64;
+    if (max) m = lanes_max<64>(m);
+    if constexpr (WG) {
+        const uint32_t wave = threadIdx.x / 64, waves = blockDim.x / 64;
         if (threadIdx.x % 64 == 0) {
             red[wave] = s;
-            red[WAVES + wave] = m;
+            if (max) red[kMostWaves + wave] = m;
         }
         __syncthreads();
-        s = red[0];
-        m = red[WAVES];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) {
-            s += red[i];
-            m = __builtin_elementwise_maximum(m, red[WAVES + i]);
-        }
+        const uint32_t l = threadIdx.x % kMostWaves;
+        s = lanes_sum<kMostWaves>(l < waves ? red[l] : 0.0f);
+        if (max) m = lanes_max<kMostWaves>(l < waves ? red[kMostWaves + l] : 0.0f);
     }
 }
 
@@ -78,37 +87,40 @@ __device__ __forceinline__ void row_reduce(float &s, float &m, float *red)
 __device__ __forceinline__ float group_max(float m, uint32_t lanes)
 {
     m = lanes_max<4>(m);   // the smallest group: 32 elements
-    if (lanes >= 8) m = __builtin_elementwise_maximum(m, lane_xor<4>(m));
-    if (lanes >= 16) m = __builtin_elementwise_maximum(m, lane_xor<8>(m));
-    if (lanes >= 32) m = __builtin_elementwise_maximum(m, lane_xor<16>(m));
-    if (lanes >= 64) m = __builtin_elementwise_maximum(m, lane_xor<32>(m));
+    if (lanes >= 8) m = lanes_max<8, 4>(m);
+    if (lanes >= 16) m = lanes_max<16, 8>(m);
+    if (lanes >= 32) m = lanes_max<32, 16>(m);
+    if (lanes >= 64) m = lanes_max<64, 32>(m);
     return m;
 }
 
+// 1 / 448 and 1 / scale are good to a unit in the last place, far inside e4m3's
+// half unit of 2^-4, and |y| / scale stays below 448 (1 + 2^-21), which rounds to
+// 448.
 __device__ __forceinline__ float e4m3_scale(float amax)
 {
-    return __builtin_elementwise_maximum(amax, 0x1p-100f) / 448.0f;
+    return __builtin_elementwise_maximum(amax, 0x1p-100f) * (1.0f / 448.0f);
 }
 
-// NP: the number of sources, 0: any (p.nsrc).  RPB rows a workgroup, each of
-// TPR threads (a wave where RPB > 1).
-template <class T, int NP, int TPR, int V, int RPB>
-__global__ __launch_bounds__(TPR *RPB) void fold_norm_kernel(NormParams p, NormSources<NP> src)
+// NP: the number of sources, 0: any (p.nsrc).  V pieces a thread; a row belongs
+// to a workgroup of at most THREADS threads, or (THREADS 0) to a wave.
+template <class T, int NP, int V, int THREADS>
+__global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm_kernel(
+    NormParams p, NormSources<NP> src)
 {
-    constexpr int kWaves = TPR / 64;
-    static_assert(RPB == 1 || kWaves == 1, "several rows a workgroup: a wave each");
+    constexpr bool kWg = THREADS != 0;
+    constexpr int RPB = kWg ? 1 : kRowsPerWg;
     constexpr int kLoads = V * Piece<T>::kWords;
-    constexpr int G = NP == 1 ? 1 : kLoads >= kInFlight ? 1 : kInFlight / kLoads;
-    __shared__ float red[2][2 * kWaves];
-    const uint32_t tid = threadIdx.x % TPR;
-    const uint32_t sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
+    constexpr int G = NP != 0 ? NP : kLoads >= kInFlight ? 1 : kInFlight / kLoads;
+    __shared__ float red[2][2 * kMostWaves];
+    const uint32_t TPR = kWg ? blockDim.x : 64, tid = kWg ? threadIdx.x : threadIdx.x % 64;
+    const uint32_t sub = kWg ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t nsrc = NP ? NP : p.nsrc;
-    // lanes without a whole piece load the row's first instead, and drop it
-    uint32_t c[V], whole[V];
+    uint32_t c[V], from[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         c[v] = piece_count(v * TPR + tid, p.hidden);
-        whole[v] = c[v] == 8 ? (v * TPR + tid) * 8 * T::kSize : 0;
+        from[v] = piece_from(v * TPR + tid, c[v], p.hidden) * T::kSize;
     }
     int turn = 0;
     for (uint64_t row = (uint64_t)blockIdx.x * RPB + sub; row < p.rows;
@@ -124,7 +136,7 @@ __global__ __launch_bounds__(TPR *RPB) void fold_norm_kernel(NormParams p, NormS
                     if (s0 + g < nsrc)
 #pragma unroll
                         for (int v = 0; v < V; ++v)
-                            in[g][v] = load_piece<T>(src(s0 + g) + at, whole[v]);
+                            in[g][v] = load_piece<T>(src(s0 + g) + at, from[v]);
 #pragma unroll
                 for (int g = 0; g < G; ++g)
                     if (s0 + g < nsrc)
@@ -140,34 +152,29 @@ __global__ __launch_bounds__(TPR *RPB) void fold_norm_kernel(NormParams p, NormS
             Piece<T> r[V];
             if (res)
 #pragma unroll
-                for (int v = 0; v < V; ++v) r[v] = load_piece<T>(res, whole[v]);
-            if constexpr (NP != 0) {
+                for (int v = 0; v < V; ++v) r[v] = load_piece<T>(res, from[v]);
+            if constexpr (NP != 0) fold(0);
+            else for (uint32_t s0 = 0; s0 < nsrc; s0 += G) fold(s0);
 #pragma unroll
-                for (uint32_t s0 = 0; s0 < NP; s0 += G) fold(s0);
-            } else {
-                for (uint32_t s0 = 0; s0 < nsrc; s0 += G) fold(s0);
-            }
-            if (res)
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
+            for (int v = 0; v < V; ++v) {
+                if (res) {
                     float x[8];
                     up_piece<T>(r[v], x);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) h[v][j] += x[j];
                 }
-        }
+                settle(h[v], c[v], p.hidden);
+            }
+        } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (c[v] != 8) {   // the row's end, and past it
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[v][j] = 0.0f;
-                const uint32_t off = (v * TPR + tid) * 8 * T::kSize;
-                for (uint32_t s = 0; c[v] != 0 && s <= nsrc; ++s) {
+            for (int v = 0; v < V; ++v) {
+                up_short<T>(src(0) + at, c[v], h[v]);
+                for (uint32_t s = 1; s <= nsrc; ++s) {
                     float x[8];
                     if (s == nsrc && !res) break;
-                    up_short<T>(s < nsrc ? src(s) + at : res, off, c[v], x);
+                    up_short<T>(s < nsrc ? src(s) + at : res, c[v], x);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) h[v][j] = s == 0 ? x[j] : h[v][j] + x[j];
+                    for (int j = 0; j < 8; ++j) h[v][j] += x[j];
                 }
             }
         }
@@ -176,18 +183,19 @@ __global__ __launch_bounds__(TPR *RPB) void fold_norm_kernel(NormParams p, NormS
 #pragma unroll
         for (int v = 0; v < V; ++v) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s += h[v][j] * h[v][j];
+            for (int j = 0; j < 8; ++j) s = __builtin_fmaf(h[v][j], h[v][j], s);
             if (row_scale) {
                 float w[8];
-                weight_piece<T>(p.weight, p.wide_weight, 8 * (v * TPR + tid), c[v], w);
+                weight_piece<T>(p.weight, p.wide_weight, v * TPR + tid, c[v], p.hidden, w);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     m = __builtin_elementwise_maximum(m, __builtin_fabsf(h[v][j] * w[j]));
+                narrow<V>();
             }
         }
-        row_reduce<kWaves>(s, m, red[turn]);
+        row_reduce<kWg>(s, m, row_scale, red[turn]);
         turn ^= 1;   // the next row's reduction leaves this one's values alone
-        const float rstd = 1.0f / __builtin_sqrtf(s / (float)p.hidden + p.eps);
+        const float rstd = rsqrtf(s * p.inv_hidden + p.eps);
         if (p.rstd && tid == 0) p.rstd[row] = rstd;
         const float row_amax = m * rstd;
         if (row_scale && tid == 0) p.scale[row * p.scale_stride] = e4m3_scale(row_amax);
@@ -196,7 +204,7 @@ __global__ __launch_bounds__(TPR *RPB) void fold_norm_kernel(NormParams p, NormS
             const uint32_t piece = v * TPR + tid, off = piece * 8 * T::kSize;
             if (p.sum) store_piece<T>(p.sum + row * p.sum_stride, off, c[v], h[v]);
             float w[8];
-            weight_piece<T>(p.weight, p.wide_weight, 8 * piece, c[v], w);
+            weight_piece<T>(p.weight, p.wide_weight, piece, c[v], p.hidden, w);
             float a = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -209,36 +217,44 @@ __global__ __launch_bounds__(TPR *RPB) void fold_norm_kernel(NormParams p, NormS
                 const float scale = e4m3_scale(p.group ? a : row_amax);
                 if (p.group && c[v] != 0 && piece % (p.group / 8) == 0)
                     p.scale[row * p.scale_stride + piece / (p.group / 8)] = scale;
-                const float inv = 1.0f / scale;
+                const float inv = __builtin_amdgcn_rcpf(scale);
                 float y[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = h[v][j] * inv;
                 store_piece_e4m3(p.out8 + row * p.out8_stride, piece * 8, c[v], y);
             }
+            narrow<V>();
         }
     }
 }
 
-template <class T, int NP, int TPR, int V, int RPB>
-hipError_t go_norm(const NormParams &p, const void *const *srcs, hipStream_t s)
+template <class T, int NP, int V, int THREADS>
+hipError_t go_norm(const NormParams &p, const void *const *srcs, unsigned threads, hipStream_t s)
 {
     NormSources<NP> src{};
     for (uint32_t i = 0; i < p.nsrc; ++i) src.p[i] = (const char *)srcs[i];
-    const unsigned grid = grid_for((p.rows + RPB - 1) / RPB);
-    return launch_kernel(fold_norm_kernel<T, NP, TPR, V, RPB>, dim3(grid), dim3(TPR * RPB), 0, s, p,
-                         src);
+    const unsigned rows = THREADS ? 1 : kRowsPerWg;
+    return launch_kernel(fold_norm_kernel<T, NP, V, THREADS>,
+                         dim3(grid_for((p.rows + rows - 1) / rows)),
+                         dim3(THREADS ? threads : 64 * kRowsPerWg), 0, s, p, src);
 }
 
+// Threads for `pieces` pieces of a row, V each, in whole waves.
+unsigned row_threads(uint32_t pieces, uint32_t v) { return (pieces + 64 * v - 1) / (64 * v) * 64; }
+
+// One piece a thread, so that a row's loads are all on their way at once; two
+// where few sources would leave a thread few loads, and there are rows enough to
+// fill the chip all the same (8192 x 4096 bf16, one source, 8-bit output: 47 us
+// against 51; 1999 x 5003 fp16, two sources 22 / 24; eight sources 134 / 130).
 template <class T, int NP>
 hipError_t go_norm_shape(const NormParams &p, const void *const *srcs, hipStream_t s)
 {
     const uint32_t pieces = (p.hidden + 7) / 8;
-    if (pieces <= 64) return go_norm<T, NP, 64, 1, 4>(p, srcs, s);
-    if (pieces <= 256) return go_norm<T, NP, 256, 1, 1>(p, srcs, s);
-    if (pieces <= 512) return go_norm<T, NP, 512, 1, 1>(p, srcs, s);
-    if (pieces <= 1024) return go_norm<T, NP, 1024, 1, 1>(p, srcs, s);
-    if (pieces <= 2048) return go_norm<T, NP, 1024, 2, 1>(p, srcs, s);
-    return go_norm<T, NP, 1024, 4, 1>(p, srcs, s);
+    if (pieces <= 64) return go_norm<T, NP, 1, 0>(p, srcs, 64, s);
+    const bool two = NP != 0 && pieces > 128 && p.rows > 2 * (uint64_t)device_cus();
+    if (pieces <= 1024 && !two) return go_norm<T, NP, 1, 1024>(p, srcs, row_threads(pieces, 1), s);
+    if (pieces <= 2048) return go_norm<T, NP, 2, 1024>(p, srcs, row_threads(pieces, 2), s);
+    return go_norm<T, 0, 4, 1024>(p, srcs, row_threads(pieces, 4), s);
 }
 
 // ---------------------------------------------------------------- gradient --
@@ -250,28 +266,49 @@ struct NormGradParams {
     uint64_t rows;
     uint64_t dout_stride, sum_stride, dsum_stride, dx_stride;   // bytes
     uint32_t hidden, slices, wide_weight;
+    float inv_hidden;
 };
 
 // dweight sums over rows, dx over a row: the threads that hold a row keep their
 // columns' part of dweight in registers over all rows of a slice (rows slice,
-// slice + slices, ...), so both come from one pass over dout and sum.
-template <class T, int TPR, int V, int RPB>
-__global__ __launch_bounds__(TPR *RPB) void norm_grad_kernel(NormGradParams p)
+// slice + slices, ...), so both come from one pass over dout and sum.  LEAN: rows
+// too wide for dsum and the weight to wait in registers too (V = 4).
+template <class T, int V, int THREADS, bool LEAN>
+__global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad_kernel(
+    NormGradParams p)
 {
-    constexpr int kWaves = TPR / 64;
-    __shared__ float red[2][2 * kWaves];
-    const uint32_t tid = threadIdx.x % TPR;
-    const uint32_t sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
-    uint32_t c[V], whole[V];   // as above
+    constexpr bool kWg = THREADS != 0;
+    constexpr int RPB = kWg ? 1 : kRowsPerWg;
+    __shared__ float red[2][2 * kMostWaves];
+    const uint32_t TPR = kWg ? blockDim.x : 64, tid = kWg ? threadIdx.x : threadIdx.x % 64;
+    const uint32_t sub = kWg ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    uint32_t c[V], from[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         c[v] = piece_count(v * TPR + tid, p.hidden);
-        whole[v] = c[v] == 8 ? (v * TPR + tid) * 8 * T::kSize : 0;
+        from[v] = piece_from(v * TPR + tid, c[v], p.hidden) * T::kSize;
     }
+    // a piece that was loaded, in place; rows shorter than one are read here
+    auto up = [&](const Piece<T> &in, const char *row, int v, float(&x)[8]) {
+        if (p.hidden >= 8) {
+            up_piece<T>(in, x);
+            settle(x, c[v], p.hidden);
+        } else {
+            up_short<T>(row, c[v], x);
+        }
+    };
+    auto load = [&](const char *row, int v) {
+        return p.hidden >= 8 ? load_piece<T>(row, from[v]) : Piece<T>{};
+    };
     float w[V][8];
+    auto weights = [&](int v) {
+        const char *weight = p.weight;
+        if (LEAN) __asm__ volatile("" : "+s"(weight));   // read anew
+        weight_piece<T>(weight, p.wide_weight, v * TPR + tid, c[v], p.hidden, w[v]);
+    };
+    if (!LEAN)
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        weight_piece<T>(p.weight, p.wide_weight, 8 * (v * TPR + tid), c[v], w[v]);
+        for (int v = 0; v < V; ++v) weights(v);
     int turn = 0;
     for (uint32_t slice = blockIdx.x * RPB + sub; slice < p.slices; slice += gridDim.x * RPB) {
         float dw[V][8];
@@ -284,34 +321,25 @@ __global__ __launch_bounds__(TPR *RPB) void norm_grad_kernel(NormGradParams p)
             const char *dout = p.dout + row * p.dout_stride, *sum = p.sum + row * p.sum_stride;
             const char *dsum = p.dsum ? p.dsum + row * p.dsum_stride : nullptr;
             Piece<T> a[V], b[V], d[V];
-            if (p.hidden >= 8) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    a[v] = load_piece<T>(dout, whole[v]);
-                    b[v] = load_piece<T>(sum, whole[v]);
-                    if (dsum) d[v] = load_piece<T>(dsum, whole[v]);
-                }
-            }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                if (c[v] != 8) {
-                    const uint32_t off = (v * TPR + tid) * 8 * T::kSize;
-                    a[v] = short_piece<T>(dout, off, c[v]);
-                    b[v] = short_piece<T>(sum, off, c[v]);
-                    if (dsum) d[v] = short_piece<T>(dsum, off, c[v]);
-                }
+                a[v] = load(dout, v);
+                b[v] = load(sum, v);
+                if (!LEAN && dsum) d[v] = load(dsum, v);
             }
             float s = 0.0f, unused = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float g[8], n[8];
-                up_piece<T>(a[v], g);
-                up_piece<T>(b[v], n);
+                up(a[v], dout, v, g);
+                up(b[v], sum, v, n);
+                if (LEAN) weights(v);
+                narrow<V>();
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     n[j] *= rstd;
-                    dw[v][j] += g[j] * n[j];
-                    s += (g[j] * w[v][j]) * n[j];
+                    dw[v][j] = __builtin_fmaf(g[j], n[j], dw[v][j]);
+                    s = __builtin_fmaf(g[j] * w[v][j], n[j], s);
                 }
             }
             // converted again below: kept in 32 bits across the reduction, the
@@ -321,23 +349,25 @@ __global__ __launch_bounds__(TPR *RPB) void norm_grad_kernel(NormGradParams p)
                 opaque_piece(a[v]);
                 opaque_piece(b[v]);
             }
-            row_reduce<kWaves>(s, unused, red[turn]);
+            row_reduce<kWg>(s, unused, false, red[turn]);
             turn ^= 1;
-            const float mean = s / (float)p.hidden;
+            const float mean = s * p.inv_hidden;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float g[8], n[8];
-                up_piece<T>(a[v], g);
-                up_piece<T>(b[v], n);
+                up(a[v], dout, v, g);
+                up(b[v], sum, v, n);
+                if (LEAN) weights(v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     g[j] = rstd * (g[j] * w[v][j] - (n[j] * rstd) * mean);
                 if (dsum) {
-                    up_piece<T>(d[v], n);
+                    up(LEAN ? load(dsum, v) : d[v], dsum, v, n);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) g[j] += n[j];
                 }
                 store_piece<T>(p.dx + row * p.dx_stride, (v * TPR + tid) * 8 * T::kSize, c[v], g);
+                narrow<V>();
             }
         }
         if (p.partial) {
@@ -375,32 +405,38 @@ __global__ __launch_bounds__(kJoinColumns *kJoinParts) void norm_dweight_kernel(
     }
 }
 
-template <class T, int TPR, int V, int RPB>
-hipError_t go_grad(const NormGradParams &p, hipStream_t s)
+template <class T, int V, int THREADS, bool LEAN = false>
+hipError_t go_grad(const NormGradParams &p, unsigned threads, hipStream_t s)
 {
-    const unsigned grid = grid_for((p.slices + RPB - 1) / RPB);
-    return launch_kernel(norm_grad_kernel<T, TPR, V, RPB>, dim3(grid), dim3(TPR * RPB), 0, s, p);
+    const unsigned slices = THREADS ? 1 : kRowsPerWg;
+    return launch_kernel(norm_grad_kernel<T, V, THREADS, LEAN>,
+                         dim3(grid_for((p.slices + slices - 1) / slices)),
+                         dim3(THREADS ? threads : 64 * kRowsPerWg), 0, s, p);
 }
 
 template <class T>
 hipError_t go_grad_shape(const NormGradParams &p, hipStream_t s)
 {
     const uint32_t pieces = (p.hidden + 7) / 8;
-    if (pieces <= 64) return go_grad<T, 64, 1, 4>(p, s);
-    if (pieces <= 256) return go_grad<T, 256, 1, 1>(p, s);
-    if (pieces <= 512) return go_grad<T, 256, 2, 1>(p, s);
-    if (pieces <= 1024) return go_grad<T, 512, 2, 1>(p, s);
-    if (pieces <= 2048) return go_grad<T, 1024, 2, 1>(p, s);
-    return go_grad<T, 1024, 4, 1>(p, s);
+    if (pieces <= 64) return go_grad<T, 1, 0>(p, 64, s);
+    if (pieces <= 512) return go_grad<T, 1, 512>(p, row_threads(pieces, 1), s);
+    if (pieces <= 2048) return go_grad<T, 2, 1024>(p, row_threads(pieces, 2), s);
+    return go_grad<T, 4, 1024, true>(p, row_threads(pieces, 4), s);
 }
 
 }  // namespace
 
-// Rows of a slice share one partial row of dweight, so there are few enough for
-// their traffic to be small beside the rows' and enough to fill the chip.
-uint32_t norm_grad_slices(uint64_t rows)
+// As many slices as put 12 waves on each CU, where HBM delivers the most beside
+// three streams that are read (16384 x 4096 bf16, 8 / 12 / 16 / 24 waves: 112 / 90 /
+// 94 / 104 us), but at least 8 rows a slice, which keeps the partial sums' traffic
+// small beside the rows'.
+uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden)
 {
-    const uint64_t s = rows / 16 < 256 ? 256 : rows / 16 > 1024 ? 1024 : rows / 16;
+    const uint32_t pieces = (uint32_t)((hidden + 7) / 8);
+    const uint64_t waves = pieces <= 512 ? (pieces + 63) / 64 : pieces <= 2048 ? (pieces + 127) / 128
+                                                                               : (pieces + 255) / 256;
+    const uint64_t fill = 12 * 256 / waves, share = rows / 8 > 256 ? rows / 8 : 256;
+    const uint64_t s = fill < share ? fill : share;
     return (uint32_t)(rows < s ? rows : s);
 }
 
@@ -427,10 +463,11 @@ hipError_t launch_fold_norm(const xred_fold_norm_args &a, hipStream_t stream)
     p.group = a.group;
     p.wide_weight = a.weight_dtype == XRED_FLOAT32;
     p.eps = a.eps;
+    p.inv_hidden = 1.0f / (float)a.hidden;
     return with_dtype_among<TF32, TBF16, TF16>(a.dtype, [&](auto t) {
         using T = decltype(t);
         if (a.nsrc == 1) return go_norm_shape<T, 1>(p, a.srcs, stream);
-        if (a.nsrc == 8) return go_norm_shape<T, 8>(p, a.srcs, stream);
+        if (a.nsrc == 2) return go_norm_shape<T, 2>(p, a.srcs, stream);
         return go_norm_shape<T, 0>(p, a.srcs, stream);
     });
 }
@@ -452,7 +489,8 @@ hipError_t launch_fold_norm_grad(const xred_fold_norm_grad_args &a, hipStream_t 
     p.dsum_stride = a.dsum.stride * es;
     p.dx_stride = a.dx.stride * es;
     p.hidden = (uint32_t)a.hidden;
-    p.slices = norm_grad_slices(a.rows);
+    p.inv_hidden = 1.0f / (float)a.hidden;
+    p.slices = norm_grad_slices(a.rows, a.hidden);
     p.wide_weight = a.weight_dtype == XRED_FLOAT32;
     if (a.rows) {
         const hipError_t e = with_dtype_among<TF32, TBF16, TF16>(

@@ -6,10 +6,10 @@
 // moves 16 bytes of a 2-byte type (32 of fp32, 8 of e4m3) at a time.  Rows may
 // start at any element, so pieces are read and written with unaligned global
 // accesses, which cost no more than aligned ones where rows are aligned.  Only
-// a row's last piece may be short; one lane moves it element by element.
+// a row's last piece may be short: its lane reads the row's last 8 elements and
+// shifts them into place, so every load is a whole one, and stores it element by
+// element.
 #pragma once
-
-#include <type_traits>
 
 #include "xred_kernels.hpp"
 
@@ -65,33 +65,6 @@ __device__ __forceinline__ void opaque_piece(Piece<T> &r)
         }
 }
 
-// The first c elements of a row's last piece (c < 8, at byte `off`); 0 past them.
-template <class T>
-__device__ __forceinline__ void up_short(const char *base, uint32_t off, uint32_t c, float (&a)[8])
-{
-#pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) a[j] = j < c ? up1<T>(base + off, j) : 0.0f;
-}
-
-// The same as it lies in memory.
-template <class T>
-__device__ __forceinline__ Piece<T> short_piece(const char *base, uint32_t off, uint32_t c)
-{
-    using Bits = std::conditional_t<T::kSize == 4, uint32_t, uint16_t>;
-    constexpr uint32_t kPer = 4 / T::kSize;   // elements of a dword
-    Piece<T> r;
-#pragma unroll
-    for (uint32_t i = 0; i < 8 / kPer; ++i) {
-        uint32_t x = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < kPer; ++j)
-            if (i * kPer + j < c)
-                x |= (uint32_t)((const Bits *)(base + off))[i * kPer + j] << (16 * j);
-        r.w[i / 4][i % 4] = x;
-    }
-    return r;
-}
-
 // Elements of piece i that exist: 8, fewer at the end of the row, 0 past it.
 __device__ __forceinline__ uint32_t piece_count(uint32_t i, uint32_t n)
 {
@@ -99,6 +72,44 @@ __device__ __forceinline__ uint32_t piece_count(uint32_t i, uint32_t n)
     return at >= n ? 0u : n - at < 8 ? n - at : 8u;
 }
 
+// Where a lane with c elements of piece i reads 8 that exist (of a row of n >= 8):
+// its piece, or the row's last 8 for the short last piece (and for no piece).
+__device__ __forceinline__ uint32_t piece_from(uint32_t i, uint32_t c, uint32_t n)
+{
+    return c == 8 ? 8 * i : n - 8;
+}
+
+// What was read there as the piece: a short piece's c elements move to the front,
+// with 0 behind them.
+__device__ __forceinline__ void settle(float (&x)[8], uint32_t c, uint32_t n)
+{
+    if (c == 8) return;
+    if (n & 7) {   // the short piece's length, the same for every row
+        const uint32_t by = 8 - (n & 7);
+        if (by & 4)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = x[j + 4];
+        if (by & 2)
+#pragma unroll
+            for (int j = 0; j < 6; ++j) x[j] = x[j + 2];
+        if (by & 1)
+#pragma unroll
+            for (int j = 0; j < 7; ++j) x[j] = x[j + 1];
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) x[j] = j < c ? x[j] : 0.0f;
+}
+
+// The same of a row shorter than a piece, element by element.
+template <class T>
+__device__ __forceinline__ void up_short(const char *base, uint32_t c, float (&a)[8])
+{
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) a[j] = j < c ? up1<T>(base, j) : 0.0f;
+}
+
+// Outputs are streamed past the caches (nontemporal): beside eight streams that
+// are read, ordinary stores cost 140 us where these take 129 (8192 x 4096 bf16).
 template <class T>
 __device__ __forceinline__ void store_piece(char *base, uint32_t off, uint32_t c,
                                             const float (&a)[8])
@@ -109,8 +120,9 @@ __device__ __forceinline__ void store_piece(char *base, uint32_t off, uint32_t c
             float b[T::kVec];
 #pragma unroll
             for (int j = 0; j < T::kVec; ++j) b[j] = a[i * T::kVec + j];
-            *(__attribute__((address_space(1))) u32x4_any *)((global_out)base + off + 16 * i) =
-                down_vec<T, OpSum>(b);
+            __builtin_nontemporal_store(
+                down_vec<T, OpSum>(b),
+                (__attribute__((address_space(1))) u32x4_any *)((global_out)base + off + 16 * i));
         }
     } else {
 #pragma unroll
@@ -119,15 +131,20 @@ __device__ __forceinline__ void store_piece(char *base, uint32_t off, uint32_t c
     }
 }
 
-// The same for e4m3 (8 bytes a piece).
+// The same for e4m3 (8 bytes a piece), values that are at most 448 or NaN: the
+// conversion itself gives NaN for more.
 __device__ __forceinline__ void store_piece_e4m3(char *base, uint32_t off, uint32_t c,
                                                  const float (&a)[8])
 {
     u32x2 q;
-    q[0] = pack_fp8x4<TE4M3>(a[0], a[1], a[2], a[3]);
-    q[1] = pack_fp8x4<TE4M3>(a[4], a[5], a[6], a[7]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i], a[4 * i + 1], 0, false);
+        q[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i + 2], a[4 * i + 3], low, true);
+    }
     if (c == 8) {
-        *(__attribute__((address_space(1))) u32x2_any *)((global_out)base + off) = q;
+        __builtin_nontemporal_store(
+            q, (__attribute__((address_space(1))) u32x2_any *)((global_out)base + off));
     } else {
 #pragma unroll
         for (uint32_t j = 0; j < 8; ++j)
@@ -136,46 +153,66 @@ __device__ __forceinline__ void store_piece_e4m3(char *base, uint32_t off, uint3
 }
 
 // ------------------------------------------------------------- reductions --
-// x of the lane l ^ M, as seen by lane l (M a power of two below 64; every lane
-// of the wave takes part).
-template <int M, class X>
-__device__ __forceinline__ X lane_xor(X x)
+// The two halves of aligned sets of 2 * M lanes, each half of M lanes already
+// reduced to one value: a holds one half's, b the other's (in either order).  The
+// steps up to 16 lanes are data-parallel moves, the last two swap rows of 16 and
+// 32 lanes, so a reduction never waits for LDS.  Every lane of the wave takes part.
+struct Halves {
+    uint32_t a, b;
+};
+template <int M>
+__device__ __forceinline__ Halves halves(uint32_t x)
 {
-    static_assert(sizeof(X) == 4, "one register");
-    const int v = __builtin_bit_cast(int, x);
-    int r;
-    if constexpr (M == 1) r = __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true);        // quad 1 0 3 2
-    else if constexpr (M == 2) r = __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true);   // quad 2 3 0 1
-    else if constexpr (M == 8) r = __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true);  // row_ror 8
-    else if constexpr (M == 16 || M == 4) r = __builtin_amdgcn_ds_swizzle(v, (M << 10) | 0x1F);
-    else r = __shfl_xor(v, 32);
-    return __builtin_bit_cast(X, r);
+    const int v = (int)x;
+    if constexpr (M == 1) {          // quads 1 0 3 2
+        return {x, (uint32_t)__builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true)};
+    } else if constexpr (M == 2) {   // quads 2 3 0 1
+        return {x, (uint32_t)__builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true)};
+    } else if constexpr (M == 4) {   // 8 lanes mirrored
+        return {x, (uint32_t)__builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true)};
+    } else if constexpr (M == 8) {   // 16 lanes mirrored
+        return {x, (uint32_t)__builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, true)};
+    } else if constexpr (M == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return {r[0], r[1]};
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return {r[0], r[1]};
+    }
 }
 
-// A sum and a maximum (NaN-propagating, like every maximum here) over aligned
-// sets of N lanes; every lane has the result.  The order of the additions is
-// fixed by the lanes' places.
+// A sum and maxima (of floats: NaN-propagating, like every maximum here) over
+// aligned sets of N lanes; every lane has the result.  The order of the additions
+// is fixed by the lanes' places.
 template <int N, int M = 1>
 __device__ __forceinline__ float lanes_sum(float x)
 {
-    if constexpr (M < N) return lanes_sum<N, 2 * M>(x + lane_xor<M>(x));
-    else return x;
+    if constexpr (M < N) {
+        const Halves h = halves<M>(__float_as_uint(x));
+        return lanes_sum<N, 2 * M>(__uint_as_float(h.a) + __uint_as_float(h.b));
+    } else {
+        return x;
+    }
 }
 
 template <int N, int M = 1>
 __device__ __forceinline__ float lanes_max(float x)
 {
-    if constexpr (M < N)
-        return lanes_max<N, 2 * M>(__builtin_elementwise_maximum(x, lane_xor<M>(x)));
-    else return x;
+    if constexpr (M < N) {
+        const Halves h = halves<M>(__float_as_uint(x));
+        return lanes_max<N, 2 * M>(
+            __builtin_elementwise_maximum(__uint_as_float(h.a), __uint_as_float(h.b)));
+    } else {
+        return x;
+    }
 }
 
 template <int N, int M = 1>
 __device__ __forceinline__ int lanes_max(int x)
 {
     if constexpr (M < N) {
-        const int y = lane_xor<M>(x);
-        return lanes_max<N, 2 * M>(x > y ? x : y);
+        const Halves h = halves<M>((uint32_t)x);
+        return lanes_max<N, 2 * M>((int)h.a > (int)h.b ? (int)h.a : (int)h.b);
     } else {
         return x;
     }
