@@ -293,64 +293,65 @@ struct CombineParams {
     uint32_t hidden, topk;
 };
 
-constexpr int kCombineSlots = 8;   // rows whose loads are in flight together
-
-// One piece a lane.  Bound by HBM: k rows are read for one that is written.
-template <class T>
+// One piece a lane, the loads of SLOTS rows in flight together.  Bound by HBM: k
+// rows are read for one that is written.
+template <class T, int SLOTS>
 __global__ __launch_bounds__(64 * kItemWaves) void combine_kernel(CombineParams p)
 {
+    constexpr int N = T::kVec;
     const uint32_t lane = threadIdx.x % 64;
+    const bool whole = p.hidden >= N;   // else rows are read element by element
     for (Item it(p.items); it.token < p.items.tokens; it.next(p.items)) {
-        const uint32_t piece = it.tile * 64 + lane, c = piece_count(piece, p.hidden);
-        const uint32_t from = piece_from(piece, c, p.hidden) * T::kSize;
+        const uint32_t piece = it.tile * 64 + lane, c = piece_count<N>(piece, p.hidden);
+        const uint32_t from = piece_from<N>(piece, c, p.hidden) * T::kSize;
         const int32_t *pos = p.pos + it.token * p.topk;
         const float *weights = p.weights ? p.weights + it.token * p.topk : nullptr;
         const char *base = p.base ? p.base + it.token * p.base_stride : nullptr;
         // -0 + t is t for every t, so the fold starts from its first term
-        float acc[8];
+        float acc[N];
         bool any = base != nullptr;
         auto clear = [&] {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] = -0.0f;
+            for (int i = 0; i < N; ++i) acc[i] = -0.0f;
         };
-        auto fold = [&](const float(&x)[8], float w, bool weighted) {
+        auto fold = [&](const float(&x)[N], float w, bool weighted) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] += weighted ? w * x[i] : x[i];
+            for (int i = 0; i < N; ++i) acc[i] += weighted ? w * x[i] : x[i];
         };
         clear();
-        Piece<T> b;
-        if (base && p.hidden >= 8) b = load_piece<T>(base, from);
-        for (uint32_t j0 = 0; j0 < p.topk; j0 += kCombineSlots) {
-            Piece<T> in[kCombineSlots];
-            bool on[kCombineSlots];
-            const char *row[kCombineSlots];
+        u32x4 b;
+        if (base && whole) b = load_piece(base, from);
+        for (uint32_t j0 = 0; j0 < p.topk; j0 += SLOTS) {
+            u32x4 in[SLOTS];
+            bool on[SLOTS];
+            const char *row[SLOTS];
 #pragma unroll
-            for (int g = 0; g < kCombineSlots; ++g) {
+            for (int g = 0; g < SLOTS; ++g) {
                 const int32_t at = j0 + g < p.topk ? sload(pos + j0 + g) : -1;
                 on[g] = at >= 0 && (uint64_t)at < p.y_rows;
                 row[g] = p.y + (on[g] ? (uint64_t)at * p.y_stride : 0);
-                if (on[g] && p.hidden >= 8) in[g] = load_piece<T>(row[g], from);
+                if (on[g] && whole) in[g] = load_piece(row[g], from);
             }
-            float x[8];
+            float x[N];
             if (j0 == 0 && base) {
-                if (p.hidden >= 8) up_piece<T>(b, x);
+                if (whole) up_vec<T>(b, x);
                 else up_short<T>(base, c, x);
                 fold(x, 1.0f, false);
             }
 #pragma unroll
-            for (int g = 0; g < kCombineSlots; ++g)
+            for (int g = 0; g < SLOTS; ++g)
                 if (on[g]) {
                     any = true;
-                    if (p.hidden >= 8) up_piece<T>(in[g], x);
+                    if (whole) up_vec<T>(in[g], x);
                     else up_short<T>(row[g], c, x);
                     fold(x, weights ? sload(weights + j0 + g) : 1.0f, weights != nullptr);
                 }
         }
         if (!any)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
-        if (p.hidden >= 8) settle(acc, c, p.hidden);
-        store_piece<T>(p.out + it.token * p.out_stride, piece * 8 * T::kSize, c, acc);
+            for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+        if (whole) settle<N>(acc, c, p.hidden);
+        store_piece<T>(p.out + it.token * p.out_stride, piece * 16, c, acc);
     }
 }
 
@@ -365,104 +366,117 @@ struct CombineGradParams {
     uint32_t hidden, topk;
 };
 
-// TPR threads a token, RPB tokens a workgroup (a wave each where RPB > 1): dout's
-// pieces are read once for kCombineSlots slots, whose rows' dot products with
-// dout stay in registers until the row's end.
-template <class T, int TPR, int RPB>
-__global__ __launch_bounds__(TPR *RPB) void combine_grad_kernel(CombineGradParams p)
+// A workgroup of at most THREADS threads a token, or (THREADS 0) a wave: dout's
+// pieces are read once for SLOTS slots, whose rows' dot products with dout stay in
+// registers until the row's end.  As many threads as pieces where that fits, so
+// that a workgroup's loads all come before its stores: a wait for loads waits for
+// the stores before them too.
+template <class T, int SLOTS, int THREADS>
+__global__ __launch_bounds__(THREADS ? THREADS : 64 * kItemWaves) void combine_grad_kernel(
+    CombineGradParams p)
 {
-    constexpr int kWaves = TPR / 64;
-    __shared__ float red[2][kWaves][kCombineSlots];
-    const uint32_t tid = threadIdx.x % TPR;
-    const uint32_t sub = RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0;
-    const uint32_t pieces = (p.hidden + 7) / 8;
+    constexpr bool kWg = THREADS != 0;
+    constexpr int N = T::kVec, kMostWaves = 16;
+    __shared__ float red[2][kWg ? kMostWaves : 1][SLOTS];
+    const uint32_t step = kWg ? blockDim.x : 64, tid = threadIdx.x % step;
+    const uint32_t per_wg = kWg ? 1 : kItemWaves;
+    const uint32_t sub = kWg ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const bool whole = p.hidden >= N;
+    const uint32_t pieces = (p.hidden + N - 1) / N;
     int turn = 0;
-    for (uint64_t token = (uint64_t)blockIdx.x * RPB + sub; token < p.tokens;
-         token += (uint64_t)gridDim.x * RPB) {
+    for (uint64_t token = (uint64_t)blockIdx.x * per_wg + sub; token < p.tokens;
+         token += (uint64_t)gridDim.x * per_wg) {
         const int32_t *pos = p.pos + token * p.topk;
         const float *weights = p.weights + token * p.topk;
         const char *dout = p.dout + token * p.dout_stride;
-        for (uint32_t j0 = 0; j0 < p.topk; j0 += kCombineSlots) {
-            float dot[kCombineSlots], w[kCombineSlots];
-            uint64_t row[kCombineSlots];
-            bool on[kCombineSlots];
+        for (uint32_t j0 = 0; j0 < p.topk; j0 += SLOTS) {
+            float dot[SLOTS], w[SLOTS];
+            uint64_t row[SLOTS];
+            bool on[SLOTS];
 #pragma unroll
-            for (int g = 0; g < kCombineSlots; ++g) {
+            for (int g = 0; g < SLOTS; ++g) {
                 const int32_t at = j0 + g < p.topk ? sload(pos + j0 + g) : -1;
                 on[g] = at >= 0 && (uint64_t)at < p.y_rows;
                 row[g] = on[g] ? (uint64_t)at : 0;
                 w[g] = on[g] ? sload(weights + j0 + g) : 0.0f;
                 dot[g] = 0.0f;
             }
-            for (uint32_t i = tid; i < pieces; i += TPR) {
-                const uint32_t c = piece_count(i, p.hidden);
-                const uint32_t from = piece_from(i, c, p.hidden) * T::kSize;
-                const bool whole = p.hidden >= 8;
-                Piece<T> a, in[kCombineSlots];
+            for (uint32_t i = tid; i < pieces; i += step) {
+                const uint32_t c = piece_count<N>(i, p.hidden);
+                const uint32_t from = piece_from<N>(i, c, p.hidden) * T::kSize;
+                u32x4 a, in[SLOTS];
                 if (whole) {
-                    a = load_piece<T, true>(dout, from);
+                    a = load_piece<true>(dout, from);
                     if (p.dweights)
 #pragma unroll
-                        for (int g = 0; g < kCombineSlots; ++g)
-                            if (on[g]) in[g] = load_piece<T>(p.y + row[g] * p.y_stride, from);
+                        for (int g = 0; g < SLOTS; ++g)
+                            if (on[g]) in[g] = load_piece(p.y + row[g] * p.y_stride, from);
                 }
-                float d[8], x[8];
+                float d[N], x[N];
                 if (whole) {
-                    up_piece<T>(a, d);
-                    settle(d, c, p.hidden);
+                    up_vec<T>(a, d);
+                    settle<N>(d, c, p.hidden);
                 } else {
                     up_short<T>(dout, c, d);
                 }
                 if (p.dweights)
 #pragma unroll
-                    for (int g = 0; g < kCombineSlots; ++g)
+                    for (int g = 0; g < SLOTS; ++g)
                         if (on[g]) {
                             if (whole) {
-                                up_piece<T>(in[g], x);
-                                settle(x, c, p.hidden);
+                                up_vec<T>(in[g], x);
+                                settle<N>(x, c, p.hidden);
                             } else {
                                 up_short<T>(p.y + row[g] * p.y_stride, c, x);
                             }
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) dot[g] = __builtin_fmaf(d[e], x[e], dot[g]);
+                            for (int e = 0; e < N; ++e) dot[g] = __builtin_fmaf(d[e], x[e], dot[g]);
                         }
 #pragma unroll
-                for (int g = 0; g < kCombineSlots; ++g)
+                for (int g = 0; g < SLOTS; ++g)
                     if (on[g]) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = w[g] * d[e];
-                        store_piece<T>(p.dy + row[g] * p.dy_stride, i * 8 * T::kSize, c, x);
+                        for (int e = 0; e < N; ++e) x[e] = w[g] * d[e];
+                        store_piece<T>(p.dy + row[g] * p.dy_stride, i * 16, c, x);
                     }
             }
             if (!p.dweights) continue;
+            float sum = 0.0f;   // lane g: of slot j0 + g
+            bool valid = false;
 #pragma unroll
-            for (int g = 0; g < kCombineSlots; ++g) dot[g] = lanes_sum<64>(dot[g]);
-            if constexpr (kWaves > 1) {
-                if (tid % 64 == 0)
-#pragma unroll
-                    for (int g = 0; g < kCombineSlots; ++g) red[turn][tid / 64][g] = dot[g];
-                __syncthreads();
-#pragma unroll
-                for (int g = 0; g < kCombineSlots; ++g) {
-                    dot[g] = red[turn][0][g];
-#pragma unroll
-                    for (int k = 1; k < kWaves; ++k) dot[g] += red[turn][k][g];
-                }
-                turn ^= 1;
+            for (int g = 0; g < SLOTS; ++g) {
+                const float s = lanes_sum<64>(dot[g]);
+                sum = threadIdx.x % 64 == (uint32_t)g ? s : sum;
+                valid |= tid == (uint32_t)g && on[g];
             }
-#pragma unroll
-            for (int g = 0; g < kCombineSlots; ++g)
-                if (tid == (uint32_t)g && j0 + g < p.topk)
-                    p.dweights[token * p.topk + j0 + g] = on[g] ? dot[g] : 0.0f;
+            if constexpr (kWg) {
+                if (threadIdx.x % 64 < SLOTS) red[turn][threadIdx.x / 64][threadIdx.x % 64] = sum;
+                __syncthreads();
+                if (tid < SLOTS) {
+                    sum = red[turn][0][tid];
+                    for (uint32_t k = 1; k < blockDim.x / 64; ++k) sum += red[turn][k][tid];
+                }
+                turn ^= 1;   // the next sums leave these alone
+            }
+            if (tid < SLOTS && j0 + tid < p.topk)
+                p.dweights[token * p.topk + j0 + tid] = valid ? sum : 0.0f;
         }
     }
 }
 
-template <class T, int TPR, int RPB>
+template <class T, int SLOTS>
 hipError_t go_combine_grad(const CombineGradParams &p, hipStream_t s)
 {
-    return launch_kernel(combine_grad_kernel<T, TPR, RPB>,
-                         dim3(grid_for((p.tokens + RPB - 1) / RPB)), dim3(TPR * RPB), 0, s, p);
+    const uint32_t pieces = (p.hidden + T::kVec - 1) / T::kVec;
+    // up to two pieces a lane a wave's own row (16384 x 1024 bf16, two slots: 31 us
+    // against 36 with two waves a row)
+    if (pieces <= 128)
+        return launch_kernel(combine_grad_kernel<T, SLOTS, 0>,
+                             dim3(grid_for((p.tokens + kItemWaves - 1) / kItemWaves)),
+                             dim3(64 * kItemWaves), 0, s, p);
+    const uint32_t threads = pieces >= 1024 ? 1024 : (pieces + 63) / 64 * 64;
+    return launch_kernel(combine_grad_kernel<T, SLOTS, 1024>, dim3(grid_for(p.tokens)),
+                         dim3(threads), 0, s, p);
 }
 
 }  // namespace
@@ -533,10 +547,16 @@ hipError_t launch_combine(const xred_combine_args &a, hipStream_t stream)
     p.out_stride = a.out.stride * es;
     p.hidden = (uint32_t)a.hidden;
     p.topk = a.topk;
-    const unsigned grid = plan_items(p.items, a.tokens, (a.hidden + 511) / 512);
+    const unsigned grid = plan_items(p.items, a.tokens, (p.hidden * es + 1023) / 1024);
+    // launches of many rounds: 16 waves a CU, by an LDS reservation (12288 x 4096
+    // bf16, top 8: 165 us against 175 with all that fit; 12 to 20 waves are alike)
+    const size_t reserve = grid > 64u * (unsigned)device_cus() ? lds_per_cu() / 4 : 0;
     return with_dtype_among<TF32, TBF16, TF16>(a.dtype, [&](auto t) {
-        return launch_kernel(combine_kernel<decltype(t)>, dim3(grid), dim3(64 * kItemWaves), 0,
-                             stream, p);
+        using T = decltype(t);
+        const dim3 block(64 * kItemWaves);
+        return p.topk <= 4
+                   ? launch_kernel(combine_kernel<T, 4>, dim3(grid), block, reserve, stream, p)
+                   : launch_kernel(combine_kernel<T, 8>, dim3(grid), block, reserve, stream, p);
     });
 }
 
@@ -559,8 +579,7 @@ hipError_t launch_combine_grad(const xred_combine_grad_args &a, hipStream_t stre
     p.topk = a.topk;
     return with_dtype_among<TF32, TBF16, TF16>(a.dtype, [&](auto t) {
         using T = decltype(t);
-        if (a.hidden <= 512) return go_combine_grad<T, 64, 4>(p, stream);
-        return go_combine_grad<T, 256, 1>(p, stream);
+        return p.topk <= 4 ? go_combine_grad<T, 4>(p, stream) : go_combine_grad<T, 8>(p, stream);
     });
 }
 

@@ -37,28 +37,43 @@ struct NormParams {
 // weight's piece i (c elements of it) as binary32; ones without a weight.
 template <class T>
 __device__ __forceinline__ void weight_piece(const char *w, bool wide, uint32_t i, uint32_t c,
-                                             uint32_t n, float (&a)[8])
+                                             uint32_t n, float (&a)[T::kVec])
 {
+    constexpr int N = T::kVec;
     if (w == nullptr) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) a[j] = 1.0f;
-    } else if (n < 8) {
-        if (wide) up_short<TF32>(w, c, a);
-        else up_short<T>(w, c, a);
-    } else {
-        const uint32_t from = piece_from(i, c, n);
-        if (wide) up_piece<TF32>(load_piece<TF32, true>(w, 4 * from), a);
-        else up_piece<T>(load_piece<T, true>(w, T::kSize * from), a);
-        settle(a, c, n);
+        for (int j = 0; j < N; ++j) a[j] = 1.0f;
+        return;
     }
+    if (n < N) {
+#pragma unroll
+        for (uint32_t j = 0; j < N; ++j)
+            a[j] = j >= c ? 0.0f : wide ? up1<TF32>(w, j) : up1<T>(w, j);
+        return;
+    }
+    const uint32_t from = piece_from<N>(i, c, n);
+    if (wide) {
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) {
+            float b[4];
+            up_vec<TF32>(load_piece<true>(w, 4 * from + 16 * k), b);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[4 * k + j] = b[j];
+        }
+    } else {
+        up_vec<T>(load_piece<true>(w, T::kSize * from), a);
+    }
+    settle<N>(a, c, n);
 }
 
-// Rows of four pieces a thread leave no registers for the loads of one piece to
+// Rows of 32 elements a thread leave no registers for the loads of one piece to
 // run ahead into the work on another.
-template <int V>
+template <class T, int V>
+constexpr bool is_wide() { return V * T::kVec >= 32; }
+template <class T, int V>
 __device__ __forceinline__ void narrow()
 {
-    if constexpr (V >= 4) __builtin_amdgcn_sched_barrier(0);
+    if constexpr (is_wide<T, V>()) __builtin_amdgcn_sched_barrier(0);
 }
 
 // Sum, and with MAX a maximum of magnitudes, over the waves of a row.  WG: the
@@ -86,7 +101,7 @@ __device__ __forceinline__ void row_reduce(float &s, float &m, bool max, float *
 // The largest |y| of each lane's group of `lanes` lanes.
 __device__ __forceinline__ float group_max(float m, uint32_t lanes)
 {
-    m = lanes_max<4>(m);   // the smallest group: 32 elements
+    m = lanes_max<4>(m);   // the smallest group: 32 elements of 8 a lane
     if (lanes >= 8) m = lanes_max<8, 4>(m);
     if (lanes >= 16) m = lanes_max<16, 8>(m);
     if (lanes >= 32) m = lanes_max<32, 16>(m);
@@ -110,71 +125,74 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
 {
     constexpr bool kWg = THREADS != 0;
     constexpr int RPB = kWg ? 1 : kRowsPerWg;
-    constexpr int kLoads = V * Piece<T>::kWords;
-    constexpr int G = NP != 0 ? NP : kLoads >= kInFlight ? 1 : kInFlight / kLoads;
-    __shared__ float red[2][2 * kMostWaves];
+    constexpr int N = T::kVec;
+    constexpr int G = NP != 0 ? NP : V >= kInFlight ? 1 : kInFlight / V;
+    // groups of 512 elements of fp32 lie in two waves (go_norm sees to it that each
+    // pair is whole); a row's reduction comes between two uses of `pair`
+    constexpr bool kPairs = kWg && N == 4;
+    __shared__ float red[2][2 * kMostWaves], pair[kPairs ? V : 1][kPairs ? kMostWaves : 1];
     const uint32_t TPR = kWg ? blockDim.x : 64, tid = kWg ? threadIdx.x : threadIdx.x % 64;
     const uint32_t sub = kWg ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t nsrc = NP ? NP : p.nsrc;
     uint32_t c[V], from[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        c[v] = piece_count(v * TPR + tid, p.hidden);
-        from[v] = piece_from(v * TPR + tid, c[v], p.hidden) * T::kSize;
+        c[v] = piece_count<N>(v * TPR + tid, p.hidden);
+        from[v] = piece_from<N>(v * TPR + tid, c[v], p.hidden) * T::kSize;
     }
     int turn = 0;
     for (uint64_t row = (uint64_t)blockIdx.x * RPB + sub; row < p.rows;
          row += (uint64_t)gridDim.x * RPB) {
-        float h[V][8];
+        float h[V][N];
         const uint64_t at = row * p.src_stride;
         const char *res = p.residual ? p.residual + row * p.residual_stride : nullptr;
-        if (p.hidden >= 8) {
+        if (p.hidden >= N) {
             auto fold = [&](uint32_t s0) {
-                Piece<T> in[G][V];
+                u32x4 in[G][V];
 #pragma unroll
                 for (int g = 0; g < G; ++g)
                     if (s0 + g < nsrc)
 #pragma unroll
                         for (int v = 0; v < V; ++v)
-                            in[g][v] = load_piece<T>(src(s0 + g) + at, from[v]);
+                            in[g][v] = load_piece(src(s0 + g) + at, from[v]);
 #pragma unroll
                 for (int g = 0; g < G; ++g)
                     if (s0 + g < nsrc)
 #pragma unroll
                         for (int v = 0; v < V; ++v) {
-                            float x[8];
-                            up_piece<T>(in[g][v], x);
+                            float x[N];
+                            up_vec<T>(in[g][v], x);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
+                            for (int j = 0; j < N; ++j)
                                 h[v][j] = s0 + g == 0 ? x[j] : h[v][j] + x[j];
                         }
             };
-            Piece<T> r[V];
+            u32x4 r[V];
             if (res)
 #pragma unroll
-                for (int v = 0; v < V; ++v) r[v] = load_piece<T>(res, from[v]);
+                for (int v = 0; v < V; ++v) r[v] = load_piece(res, from[v]);
             if constexpr (NP != 0) fold(0);
             else for (uint32_t s0 = 0; s0 < nsrc; s0 += G) fold(s0);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (res) {
-                    float x[8];
-                    up_piece<T>(r[v], x);
+                    float x[N];
+                    up_vec<T>(r[v], x);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) h[v][j] += x[j];
+                    for (int j = 0; j < N; ++j) h[v][j] += x[j];
                 }
-                settle(h[v], c[v], p.hidden);
+                settle<N>(h[v], c[v], p.hidden);
             }
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 up_short<T>(src(0) + at, c[v], h[v]);
                 for (uint32_t s = 1; s <= nsrc; ++s) {
-                    float x[8];
+                    float x[N];
                     if (s == nsrc && !res) break;
                     up_short<T>(s < nsrc ? src(s) + at : res, c[v], x);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) h[v][j] += x[j];
+                    for (int j = 0; j < N; ++j) h[v][j] += x[j];
                 }
             }
         }
@@ -183,14 +201,14 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
 #pragma unroll
         for (int v = 0; v < V; ++v) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s = __builtin_fmaf(h[v][j], h[v][j], s);
+            for (int j = 0; j < N; ++j) s = __builtin_fmaf(h[v][j], h[v][j], s);
             if (row_scale) {
-                float w[8];
+                float w[N];
                 weight_piece<T>(p.weight, p.wide_weight, v * TPR + tid, c[v], p.hidden, w);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int j = 0; j < N; ++j)
                     m = __builtin_elementwise_maximum(m, __builtin_fabsf(h[v][j] * w[j]));
-                narrow<V>();
+                narrow<T, V>();
             }
         }
         row_reduce<kWg>(s, m, row_scale, red[turn]);
@@ -201,29 +219,35 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
         if (row_scale && tid == 0) p.scale[row * p.scale_stride] = e4m3_scale(row_amax);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t piece = v * TPR + tid, off = piece * 8 * T::kSize;
+            const uint32_t piece = v * TPR + tid, off = piece * 16;
             if (p.sum) store_piece<T>(p.sum + row * p.sum_stride, off, c[v], h[v]);
-            float w[8];
+            float w[N];
             weight_piece<T>(p.weight, p.wide_weight, piece, c[v], p.hidden, w);
             float a = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < N; ++j) {
                 h[v][j] = h[v][j] * (rstd * w[j]);   // one rounding of what may be subnormal
                 a = __builtin_elementwise_maximum(a, __builtin_fabsf(h[v][j]));
             }
             if (p.out) store_piece<T>(p.out + row * p.out_stride, off, c[v], h[v]);
             if (p.out8) {
-                if (p.group) a = group_max(a, p.group / 8);
+                if (p.group) a = group_max(a, p.group / N < 64 ? p.group / N : 64);
+                if constexpr (kPairs)
+                    if (p.group / N == 128) {   // a pair of waves
+                        if (tid % 64 == 0) pair[v][tid / 64] = a;
+                        __syncthreads();
+                        a = __builtin_elementwise_maximum(a, pair[v][tid / 64 ^ 1]);
+                    }
                 const float scale = e4m3_scale(p.group ? a : row_amax);
-                if (p.group && c[v] != 0 && piece % (p.group / 8) == 0)
-                    p.scale[row * p.scale_stride + piece / (p.group / 8)] = scale;
+                if (p.group && c[v] != 0 && piece % (p.group / N) == 0)
+                    p.scale[row * p.scale_stride + piece / (p.group / N)] = scale;
                 const float inv = __builtin_amdgcn_rcpf(scale);
-                float y[8];
+                float y[N];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = h[v][j] * inv;
-                store_piece_e4m3(p.out8 + row * p.out8_stride, piece * 8, c[v], y);
+                for (int j = 0; j < N; ++j) y[j] = h[v][j] * inv;
+                store_piece_e4m3<N>(p.out8 + row * p.out8_stride, piece * N, c[v], y);
             }
-            narrow<V>();
+            narrow<T, V>();
         }
     }
 }
@@ -234,6 +258,7 @@ hipError_t go_norm(const NormParams &p, const void *const *srcs, unsigned thread
     NormSources<NP> src{};
     for (uint32_t i = 0; i < p.nsrc; ++i) src.p[i] = (const char *)srcs[i];
     const unsigned rows = THREADS ? 1 : kRowsPerWg;
+    if (T::kVec == 4 && p.group == 512) threads = (threads + 127) / 128 * 128;
     return launch_kernel(fold_norm_kernel<T, NP, V, THREADS>,
                          dim3(grid_for((p.rows + rows - 1) / rows)),
                          dim3(THREADS ? threads : 64 * kRowsPerWg), 0, s, p, src);
@@ -249,13 +274,16 @@ unsigned row_threads(uint32_t pieces, uint32_t v) { return (pieces + 64 * v - 1)
 template <class T, int NP>
 hipError_t go_norm_shape(const NormParams &p, const void *const *srcs, hipStream_t s)
 {
-    const uint32_t pieces = (p.hidden + 7) / 8;
+    const uint32_t pieces = (p.hidden + T::kVec - 1) / T::kVec;
     if (pieces <= 64) return go_norm<T, NP, 1, 0>(p, srcs, 64, s);
     const bool two = NP != 0 && pieces > 128 && p.rows > 2 * (uint64_t)device_cus();
     if (pieces <= 1024 && !two) return go_norm<T, NP, 1, 1024>(p, srcs, row_threads(pieces, 1), s);
     if (pieces <= 2048) return go_norm<T, NP, 2, 1024>(p, srcs, row_threads(pieces, 2), s);
-    return go_norm<T, 0, 4, 1024>(p, srcs, row_threads(pieces, 4), s);
+    if (pieces <= 4096) return go_norm<T, 0, 4, 1024>(p, srcs, row_threads(pieces, 4), s);
+    if constexpr (T::kVec == 4) return go_norm<T, 0, 8, 1024>(p, srcs, row_threads(pieces, 8), s);
+    return hipErrorInvalidValue;
 }
+static_assert(XRED_MAX_HIDDEN <= 1024 * 32, "the widest row is 32 elements a thread");
 
 // ---------------------------------------------------------------- gradient --
 struct NormGradParams {
@@ -272,35 +300,35 @@ struct NormGradParams {
 // dweight sums over rows, dx over a row: the threads that hold a row keep their
 // columns' part of dweight in registers over all rows of a slice (rows slice,
 // slice + slices, ...), so both come from one pass over dout and sum.  LEAN: rows
-// too wide for dsum and the weight to wait in registers too (V = 4).
-template <class T, int V, int THREADS, bool LEAN>
+// too wide for dsum and the weight to wait in registers too.
+template <class T, int V, int THREADS>
 __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad_kernel(
     NormGradParams p)
 {
-    constexpr bool kWg = THREADS != 0;
-    constexpr int RPB = kWg ? 1 : kRowsPerWg;
+    constexpr bool kWg = THREADS != 0, LEAN = is_wide<T, V>();
+    constexpr int N = T::kVec, RPB = kWg ? 1 : kRowsPerWg;
     __shared__ float red[2][2 * kMostWaves];
     const uint32_t TPR = kWg ? blockDim.x : 64, tid = kWg ? threadIdx.x : threadIdx.x % 64;
     const uint32_t sub = kWg ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     uint32_t c[V], from[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        c[v] = piece_count(v * TPR + tid, p.hidden);
-        from[v] = piece_from(v * TPR + tid, c[v], p.hidden) * T::kSize;
+        c[v] = piece_count<N>(v * TPR + tid, p.hidden);
+        from[v] = piece_from<N>(v * TPR + tid, c[v], p.hidden) * T::kSize;
     }
     // a piece that was loaded, in place; rows shorter than one are read here
-    auto up = [&](const Piece<T> &in, const char *row, int v, float(&x)[8]) {
-        if (p.hidden >= 8) {
-            up_piece<T>(in, x);
-            settle(x, c[v], p.hidden);
+    auto up = [&](u32x4 in, const char *row, int v, float(&x)[N]) {
+        if (p.hidden >= N) {
+            up_vec<T>(in, x);
+            settle<N>(x, c[v], p.hidden);
         } else {
             up_short<T>(row, c[v], x);
         }
     };
     auto load = [&](const char *row, int v) {
-        return p.hidden >= 8 ? load_piece<T>(row, from[v]) : Piece<T>{};
+        return p.hidden >= N ? load_piece(row, from[v]) : u32x4{};
     };
-    float w[V][8];
+    float w[V][N];
     auto weights = [&](int v) {
         const char *weight = p.weight;
         if (LEAN) __asm__ volatile("" : "+s"(weight));   // read anew
@@ -311,16 +339,16 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad
         for (int v = 0; v < V; ++v) weights(v);
     int turn = 0;
     for (uint32_t slice = blockIdx.x * RPB + sub; slice < p.slices; slice += gridDim.x * RPB) {
-        float dw[V][8];
+        float dw[V][N];
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) dw[v][j] = 0.0f;
+            for (int j = 0; j < N; ++j) dw[v][j] = 0.0f;
         for (uint64_t row = slice; row < p.rows; row += p.slices) {
             const float rstd = p.rstd[row];
             const char *dout = p.dout + row * p.dout_stride, *sum = p.sum + row * p.sum_stride;
             const char *dsum = p.dsum ? p.dsum + row * p.dsum_stride : nullptr;
-            Piece<T> a[V], b[V], d[V];
+            u32x4 a[V], b[V], d[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 a[v] = load(dout, v);
@@ -330,13 +358,13 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad
             float s = 0.0f, unused = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                float g[8], n[8];
+                float g[N], n[N];
                 up(a[v], dout, v, g);
                 up(b[v], sum, v, n);
                 if (LEAN) weights(v);
-                narrow<V>();
+                narrow<T, V>();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < N; ++j) {
                     n[j] *= rstd;
                     dw[v][j] = __builtin_fmaf(g[j], n[j], dw[v][j]);
                     s = __builtin_fmaf(g[j] * w[v][j], n[j], s);
@@ -354,27 +382,33 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad
             const float mean = s * p.inv_hidden;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                float g[8], n[8];
+                float g[N], n[N];
                 up(a[v], dout, v, g);
                 up(b[v], sum, v, n);
                 if (LEAN) weights(v);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int j = 0; j < N; ++j)
                     g[j] = rstd * (g[j] * w[v][j] - (n[j] * rstd) * mean);
                 if (dsum) {
                     up(LEAN ? load(dsum, v) : d[v], dsum, v, n);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) g[j] += n[j];
+                    for (int j = 0; j < N; ++j) g[j] += n[j];
                 }
-                store_piece<T>(p.dx + row * p.dx_stride, (v * TPR + tid) * 8 * T::kSize, c[v], g);
-                narrow<V>();
+                store_piece<T>(p.dx + row * p.dx_stride, (v * TPR + tid) * 16, c[v], g);
+                narrow<T, V>();
             }
         }
         if (p.partial) {
+            char *part = (char *)(p.partial + (uint64_t)slice * p.hidden);
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                store_piece<TF32>((char *)(p.partial + (uint64_t)slice * p.hidden),
-                                  (v * TPR + tid) * 32, c[v], dw[v]);
+#pragma unroll
+                for (int k = 0; k < N / 4; ++k) {
+                    const uint32_t at = (v * TPR + tid) * N + 4 * k;
+                    const float four[4] = {dw[v][4 * k], dw[v][4 * k + 1], dw[v][4 * k + 2],
+                                           dw[v][4 * k + 3]};
+                    store_piece<TF32>(part, at * 4, piece_count<4>(at / 4, p.hidden), four);
+                }
         }
     }
 }
@@ -405,23 +439,33 @@ __global__ __launch_bounds__(kJoinColumns *kJoinParts) void norm_dweight_kernel(
     }
 }
 
-template <class T, int V, int THREADS, bool LEAN = false>
+template <class T, int V, int THREADS>
 hipError_t go_grad(const NormGradParams &p, unsigned threads, hipStream_t s)
 {
     const unsigned slices = THREADS ? 1 : kRowsPerWg;
-    return launch_kernel(norm_grad_kernel<T, V, THREADS, LEAN>,
+    return launch_kernel(norm_grad_kernel<T, V, THREADS>,
                          dim3(grid_for((p.slices + slices - 1) / slices)),
                          dim3(THREADS ? threads : 64 * kRowsPerWg), 0, s, p);
+}
+
+// Pieces a thread of a row's workgroup, for rows past a wave.
+uint32_t grad_pieces(uint32_t pieces)
+{
+    return pieces <= 512 ? 1 : pieces <= 2048 ? 2 : pieces <= 4096 ? 4 : 8;
 }
 
 template <class T>
 hipError_t go_grad_shape(const NormGradParams &p, hipStream_t s)
 {
-    const uint32_t pieces = (p.hidden + 7) / 8;
+    const uint32_t pieces = (p.hidden + T::kVec - 1) / T::kVec;
     if (pieces <= 64) return go_grad<T, 1, 0>(p, 64, s);
-    if (pieces <= 512) return go_grad<T, 1, 512>(p, row_threads(pieces, 1), s);
-    if (pieces <= 2048) return go_grad<T, 2, 1024>(p, row_threads(pieces, 2), s);
-    return go_grad<T, 4, 1024, true>(p, row_threads(pieces, 4), s);
+    const uint32_t v = grad_pieces(pieces);
+    const unsigned threads = row_threads(pieces, v);
+    if (v == 1) return go_grad<T, 1, 512>(p, threads, s);
+    if (v == 2) return go_grad<T, 2, 1024>(p, threads, s);
+    if (v == 4) return go_grad<T, 4, 1024>(p, threads, s);
+    if constexpr (T::kVec == 4) return go_grad<T, 8, 1024>(p, threads, s);
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -429,13 +473,13 @@ hipError_t go_grad_shape(const NormGradParams &p, hipStream_t s)
 // As many slices as put 12 waves on each CU, where HBM delivers the most beside
 // three streams that are read (16384 x 4096 bf16, 8 / 12 / 16 / 24 waves: 112 / 90 /
 // 94 / 104 us), but at least 8 rows a slice, which keeps the partial sums' traffic
-// small beside the rows'.
+// small beside the rows'.  (Counted for 2-byte types; rows of fp32 take up to
+// twice the waves.)
 uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden)
 {
     const uint32_t pieces = (uint32_t)((hidden + 7) / 8);
-    const uint64_t waves = pieces <= 512 ? (pieces + 63) / 64 : pieces <= 2048 ? (pieces + 127) / 128
-                                                                               : (pieces + 255) / 256;
-    const uint64_t fill = 12 * 256 / waves, share = rows / 8 > 256 ? rows / 8 : 256;
+    const uint64_t waves = row_threads(pieces, grad_pieces(pieces)) / 64;
+    const uint64_t fill = 12 * 256 / (waves ? waves : 1), share = rows / 8 > 256 ? rows / 8 : 256;
     const uint64_t s = fill < share ? fill : share;
     return (uint32_t)(rows < s ? rows : s);
 }

@@ -1,14 +1,14 @@
 // xred_rows.hpp -- device helpers shared by the kernels that work on rows
-// (norm, dispatch, combine): pieces of 8 elements at any element alignment,
-// and reductions over a wave and a workgroup.
+// (norm, dispatch, combine): pieces of 16 bytes at any element alignment, and
+// reductions over a wave and a workgroup.
 //
-// A row is cut into pieces of 8 elements; a lane owns whole pieces, so a lane
-// moves 16 bytes of a 2-byte type (32 of fp32, 8 of e4m3) at a time.  Rows may
-// start at any element, so pieces are read and written with unaligned global
-// accesses, which cost no more than aligned ones where rows are aligned.  Only
-// a row's last piece may be short: its lane reads the row's last 8 elements and
-// shifts them into place, so every load is a whole one, and stores it element by
-// element.
+// A row is cut into pieces of one 16-byte vector, N = 8 elements of a 2-byte type
+// or 4 of fp32; a lane owns whole pieces, and neighbouring lanes neighbouring
+// pieces.  Rows may start at any element, so pieces are read and written with
+// unaligned global accesses, which cost no more than aligned ones where rows are
+// aligned.  Only a row's last piece may be short: its lane reads the row's last N
+// elements and shifts them into place, so every load is a whole one, and stores it
+// element by element.
 #pragma once
 
 #include "xred_kernels.hpp"
@@ -17,137 +17,112 @@ namespace xred {
 
 typedef __attribute__((address_space(1))) char *global_out;
 
-// 8 consecutive elements as they lie in memory.
-template <class T>
-struct Piece {
-    static constexpr int kWords = T::kSize * 8 / 16;
-    u32x4 w[kWords];
-};
-
 // off: bytes from base, the same base in every lane.  KEEP: the data is read
 // again soon (by other workgroups), else it is streamed.
-template <class T, bool KEEP = false>
-__device__ __forceinline__ Piece<T> load_piece(const char *base, uint32_t off)
+template <bool KEEP = false>
+__device__ __forceinline__ u32x4 load_piece(const char *base, uint32_t off)
 {
-    Piece<T> r;
-#pragma unroll
-    for (int i = 0; i < Piece<T>::kWords; ++i) {
-        const auto *p =
-            (const __attribute__((address_space(1))) u32x4_any *)((global_bytes)base + off + 16 * i);
-        r.w[i] = KEEP ? *p : __builtin_nontemporal_load(p);
-    }
-    return r;
-}
-
-template <class T>
-__device__ __forceinline__ void up_piece(const Piece<T> &r, float (&a)[8])
-{
-#pragma unroll
-    for (int i = 0; i < Piece<T>::kWords; ++i) {
-        float b[T::kVec];
-        up_vec<T>(r.w[i], b);
-#pragma unroll
-        for (int j = 0; j < T::kVec; ++j) a[i * T::kVec + j] = b[j];
-    }
+    const auto *p = (const __attribute__((address_space(1))) u32x4_any *)((global_bytes)base + off);
+    return KEEP ? *p : __builtin_nontemporal_load(p);
 }
 
 // The same values, hidden from the optimiser.
-template <class T>
-__device__ __forceinline__ void opaque_piece(Piece<T> &r)
+__device__ __forceinline__ void opaque_piece(u32x4 &r)
 {
 #pragma unroll
-    for (int i = 0; i < Piece<T>::kWords; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t x = r.w[i][j];
-            __asm__ volatile("" : "+v"(x));
-            r.w[i][j] = x;
-        }
+    for (int j = 0; j < 4; ++j) {
+        uint32_t x = r[j];
+        __asm__ volatile("" : "+v"(x));
+        r[j] = x;
+    }
 }
 
-// Elements of piece i that exist: 8, fewer at the end of the row, 0 past it.
+// Elements of piece i of a row of n: N, fewer at the end of the row, 0 past it.
+template <int N>
 __device__ __forceinline__ uint32_t piece_count(uint32_t i, uint32_t n)
 {
-    const uint32_t at = 8 * i;
-    return at >= n ? 0u : n - at < 8 ? n - at : 8u;
+    const uint32_t at = N * i;
+    return at >= n ? 0u : n - at < N ? n - at : (uint32_t)N;
 }
 
-// Where a lane with c elements of piece i reads 8 that exist (of a row of n >= 8):
-// its piece, or the row's last 8 for the short last piece (and for no piece).
+// Where a lane with c elements of piece i reads N that exist (of a row of n >= N):
+// its piece, or the row's last N for the short last piece (and for no piece).
+template <int N>
 __device__ __forceinline__ uint32_t piece_from(uint32_t i, uint32_t c, uint32_t n)
 {
-    return c == 8 ? 8 * i : n - 8;
+    return c == N ? N * i : n - N;
 }
 
 // What was read there as the piece: a short piece's c elements move to the front,
 // with 0 behind them.
-__device__ __forceinline__ void settle(float (&x)[8], uint32_t c, uint32_t n)
+template <int N>
+__device__ __forceinline__ void settle(float (&x)[N], uint32_t c, uint32_t n)
 {
-    if (c == 8) return;
-    if (n & 7) {   // the short piece's length, the same for every row
-        const uint32_t by = 8 - (n & 7);
-        if (by & 4)
+    if (c == N) return;
+    if (n % N) {   // the short piece's length, the same for every row
+        const uint32_t by = N - n % N;
+        if (N == 8 && (by & 4))
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = x[j + 4];
+            for (int j = 0; j < N - 4; ++j) x[j] = x[j + 4];
         if (by & 2)
 #pragma unroll
-            for (int j = 0; j < 6; ++j) x[j] = x[j + 2];
+            for (int j = 0; j < N - 2; ++j) x[j] = x[j + 2];
         if (by & 1)
 #pragma unroll
-            for (int j = 0; j < 7; ++j) x[j] = x[j + 1];
+            for (int j = 0; j < N - 1; ++j) x[j] = x[j + 1];
     }
 #pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) x[j] = j < c ? x[j] : 0.0f;
+    for (uint32_t j = 0; j < N; ++j) x[j] = j < c ? x[j] : 0.0f;
 }
 
 // The same of a row shorter than a piece, element by element.
 template <class T>
-__device__ __forceinline__ void up_short(const char *base, uint32_t c, float (&a)[8])
+__device__ __forceinline__ void up_short(const char *base, uint32_t c, float (&a)[T::kVec])
 {
 #pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) a[j] = j < c ? up1<T>(base, j) : 0.0f;
+    for (uint32_t j = 0; j < T::kVec; ++j) a[j] = j < c ? up1<T>(base, j) : 0.0f;
 }
 
 // Outputs are streamed past the caches (nontemporal): beside eight streams that
 // are read, ordinary stores cost 140 us where these take 129 (8192 x 4096 bf16).
 template <class T>
 __device__ __forceinline__ void store_piece(char *base, uint32_t off, uint32_t c,
-                                            const float (&a)[8])
+                                            const float (&a)[T::kVec])
 {
-    if (c == 8) {
-#pragma unroll
-        for (int i = 0; i < Piece<T>::kWords; ++i) {
-            float b[T::kVec];
-#pragma unroll
-            for (int j = 0; j < T::kVec; ++j) b[j] = a[i * T::kVec + j];
-            __builtin_nontemporal_store(
-                down_vec<T, OpSum>(b),
-                (__attribute__((address_space(1))) u32x4_any *)((global_out)base + off + 16 * i));
-        }
+    if (c == T::kVec) {
+        __builtin_nontemporal_store(
+            down_vec<T, OpSum>(a),
+            (__attribute__((address_space(1))) u32x4_any *)((global_out)base + off));
     } else {
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j)
+        for (uint32_t j = 0; j < T::kVec; ++j)
             if (j < c) down1<T, OpSum>(base + off, j, a[j]);
     }
 }
 
-// The same for e4m3 (8 bytes a piece), values that are at most 448 or NaN: the
+// The same for e4m3 (a byte an element), values that are at most 448 or NaN: the
 // conversion itself gives NaN for more.
+template <int N>
 __device__ __forceinline__ void store_piece_e4m3(char *base, uint32_t off, uint32_t c,
-                                                 const float (&a)[8])
+                                                 const float (&a)[N])
 {
-    u32x2 q;
+    uint32_t q[N / 4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < N / 4; ++i) {
         const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i], a[4 * i + 1], 0, false);
         q[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a[4 * i + 2], a[4 * i + 3], low, true);
     }
-    if (c == 8) {
-        __builtin_nontemporal_store(
-            q, (__attribute__((address_space(1))) u32x2_any *)((global_out)base + off));
+    if (c == N) {
+        if constexpr (N == 8)
+            __builtin_nontemporal_store(
+                u32x2{q[0], q[1]},
+                (__attribute__((address_space(1))) u32x2_any *)((global_out)base + off));
+        else
+            __builtin_nontemporal_store(
+                q[0], (__attribute__((address_space(1))) u32_any *)((global_out)base + off));
     } else {
 #pragma unroll
-        for (uint32_t j = 0; j < 8; ++j)
+        for (uint32_t j = 0; j < N; ++j)
             if (j < c) base[off + j] = (char)(q[j / 4] >> (8 * (j % 4)));
     }
 }
