@@ -239,11 +239,12 @@ struct DispatchParams {
     uint32_t bytes, topk, scale_columns;
 };
 
-constexpr int kCopyVecs = 2;   // vectors a lane of a tile
-
-// A row is read once and written topk times.  Its last vector ends with the row,
-// overlapping the one before it (both write the same bytes there), so there is
-// no tail but in rows shorter than a vector.
+// One vector of a row a lane: it is read once and written topk times.  A row's last
+// vector ends with the row, overlapping the one before it (both write the same
+// bytes there), so there is no tail but in rows shorter than a vector.  STREAM:
+// rows on the 16-byte grid are written nontemporally; off it neighbouring vectors
+// share lines, which ordinary stores join in L2.
+template <bool STREAM>
 __global__ __launch_bounds__(64 * kItemWaves) void dispatch_kernel(DispatchParams p)
 {
     const uint32_t lane = threadIdx.x % 64;
@@ -251,26 +252,20 @@ __global__ __launch_bounds__(64 * kItemWaves) void dispatch_kernel(DispatchParam
     for (Item it(p.items); it.token < p.items.tokens; it.next(p.items)) {
         const char *x = p.x + it.token * p.stride;
         const int32_t *pos = p.pos + it.token * p.topk;
-        u32x4 v[kCopyVecs];
-        uint32_t off[kCopyVecs];
-        bool on[kCopyVecs];
-#pragma unroll
-        for (int u = 0; u < kCopyVecs; ++u) {
-            const uint32_t i = (it.tile * kCopyVecs + u) * 64 + lane;
-            on[u] = i < vecs && p.bytes >= 16;
-            off[u] = i + 1 < vecs ? 16 * i : p.bytes - 16;
-            if (on[u])
-                v[u] = __builtin_nontemporal_load(
-                    (const __attribute__((address_space(1))) u32x4_any *)((global_bytes)x + off[u]));
-        }
+        const uint32_t i = it.tile * 64 + lane;
+        const bool on = i < vecs && p.bytes >= 16;
+        const uint32_t off = i + 1 < vecs ? 16 * i : p.bytes - 16;
+        u32x4 v;
+        if (on) v = load_piece(x, off);
         for (uint32_t j = 0; j < p.topk; ++j) {
             const int32_t to = sload(pos + j);
             if (to < 0 || (uint64_t)to >= p.out_rows) continue;
             char *out = p.out + (uint64_t)to * p.out_stride;
-#pragma unroll
-            for (int u = 0; u < kCopyVecs; ++u)
-                if (on[u])
-                    *(__attribute__((address_space(1))) u32x4_any *)((global_out)out + off[u]) = v[u];
+            if (on) {
+                auto *o = (__attribute__((address_space(1))) u32x4_any *)((global_out)out + off);
+                if (STREAM) __builtin_nontemporal_store(v, o);
+                else *o = v;
+            }
             if (p.bytes < 16 && lane < p.bytes) out[lane] = x[lane];
             if (it.tile == 0 && p.scale) {
                 const float *s = p.scale + it.token * p.scale_stride;
@@ -527,9 +522,14 @@ hipError_t launch_dispatch(const xred_dispatch_args &a, hipStream_t stream)
     p.bytes = (uint32_t)(a.hidden * es);
     p.topk = a.topk;
     p.scale_columns = (uint32_t)a.scale_columns;
-    constexpr uint64_t tile = 64 * kCopyVecs * 16;
-    const unsigned grid = plan_items(p.items, a.tokens, (p.bytes + tile - 1) / tile);
-    return launch_kernel(dispatch_kernel, dim3(grid), dim3(64 * kItemWaves), 0, stream, p);
+    const unsigned grid = plan_items(p.items, a.tokens, (p.bytes + 1023) / 1024);
+    const bool grid16 = ((uintptr_t)p.out | p.out_stride | p.bytes) % 16 == 0;
+    // On the grid, launches of many rounds: 20 waves a CU, by an LDS reservation
+    // (16384 x 4096 e4m3, top 8: nontemporal 105 us, uncapped 110, ordinary stores
+    // 112; rows of 4099: ordinary 140, nontemporal 150, ordinary capped 178).
+    const size_t reserve = grid16 && grid > 64u * (unsigned)device_cus() ? lds_per_cu() / 5 : 0;
+    return launch_kernel(grid16 ? dispatch_kernel<true> : dispatch_kernel<false>, dim3(grid),
+                         dim3(64 * kItemWaves), reserve, stream, p);
 }
 
 hipError_t launch_combine(const xred_combine_args &a, hipStream_t stream)
