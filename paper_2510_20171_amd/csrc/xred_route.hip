@@ -2,11 +2,15 @@
 // of its weights (xred_route_grad).
 //
 // L lanes share a token, V consecutive experts each, so a wave routes 64 / L
-// tokens at once and a row is read once, into registers.  The choice is topk
-// rounds of "largest key, lowest index": keys are mapped to integers of the
-// same order, each lane keeps the largest of its own, and the lanes of a token
-// agree by a butterfly of cross-lane maxima.  Experts lie in lane order, so the
-// lowest lane that holds the maximum holds the lowest index.
+// tokens at once and a row is read once, into registers.  Experts lie in lane
+// order, so among equal keys the lowest lane holds the lowest index.
+//
+// Routing is bound by its arithmetic, not by HBM, so the choice avoids rounds of
+// "find the largest, take it out", each of which visits every key.  The topk-th
+// largest of a few lanes' best keys bounds the choice from below: topk keys are
+// at least that large.  The few keys that reach it are gathered, one a lane, and
+// each finds its place by counting the keys before it.  Rows for which that fails
+// (a NaN, more than 16 keys that reach the bound) take the rounds.
 #include "xred_layer.hpp"
 #include "xred_rows.hpp"
 
@@ -24,6 +28,7 @@ struct RouteParams {
     float *weights;
     uint64_t tokens, stride;   // stride in bytes
     uint32_t experts, topk, groups, group_topk, group_score, per_group, per_group_inv;
+    uint32_t group_lanes;   // lanes of a group, 0 unless whole ones and a power of two
     uint32_t renorm;
     float scale;
 };
@@ -41,20 +46,18 @@ __device__ __forceinline__ float value_of(int k)
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
 
-// The first V experts from e on of a row: -inf past the last.
+// The first V experts from e on of a row: -inf past the last.  all: every lane's
+// V experts are there.
 template <class T, int V>
-__device__ __forceinline__ void load_logits(const char *row, uint32_t e, uint32_t experts,
+__device__ __forceinline__ void load_logits(const char *row, uint32_t e, uint32_t experts, bool all,
                                             float (&x)[V])
 {
     if constexpr (V % T::kVec == 0) {
-        if (e + V <= experts) {
+        if (all || e + V <= experts) {
 #pragma unroll
             for (int i = 0; i < V / T::kVec; ++i) {
                 float a[T::kVec];
-                up_vec<T>(__builtin_nontemporal_load(
-                              (const __attribute__((address_space(1))) u32x4_any *)(
-                                  (global_bytes)row + e * T::kSize + 16 * i)),
-                          a);
+                up_vec<T>(load_piece(row, e * T::kSize + 16 * i), a);
 #pragma unroll
                 for (int j = 0; j < T::kVec; ++j) x[i * T::kVec + j] = a[j];
             }
@@ -62,7 +65,11 @@ __device__ __forceinline__ void load_logits(const char *row, uint32_t e, uint32_
         }
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = e + i < experts ? up1<T>(row, e + i) : -__builtin_inff();
+    for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
+    if (e >= experts) return;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (e + i < experts) x[i] = up1<T>(row, e + i);
 }
 
 // Of the lanes of each set of L that have `on`, the lowest (64 if none).
@@ -74,115 +81,332 @@ __device__ __forceinline__ uint32_t lowest_lane(bool on, uint32_t first)
     return own ? (uint32_t)__builtin_ctzll(own) : 64u;
 }
 
+// How many of a row's 16 lanes come before this one: with a larger key, or with
+// the same key and a lower place.  (x before y if x + 1 > y where x's place is the
+// lower, else if x > y.)
+template <int D = 1>
+__device__ __forceinline__ uint32_t place_in_row(int key, uint32_t rank = 0)
+{
+    if constexpr (D < 16) {
+        // the key D lanes below, around the row
+        const int other = __builtin_amdgcn_mov_dpp(key, 0x120 + D, 0xF, 0xF, true);
+        const int lower = threadIdx.x % 16 >= D ? 1 : 0;
+        return place_in_row<D + 1>(key, rank + (other + lower > key ? 1 : 0));
+    } else {
+        return rank;
+    }
+}
+
+// Sum of x over the lanes below this one in its set of L, and over all of them.
+template <int L>
+__device__ __forceinline__ void lanes_before(uint32_t x, uint32_t &before, uint32_t &all)
+{
+    uint32_t s = x;   // row_shr 1, 2, 4, 8; then the rows before
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x111, 0xF, 0xF, true);
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x112, 0xF, 0xF, true);
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x114, 0xF, 0xF, true);
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x118, 0xF, 0xF, true);
+    if constexpr (L == 64) {
+        s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x142, 0xA, 0xF, false);
+        s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x143, 0xC, 0xF, false);
+    }
+    before = s - x;
+    all = (uint32_t)lanes_max<L>((int)s);
+}
+
+// The best two of V keys (-inf where there are fewer); a is NaN if one of them is.
+template <int V>
+__device__ __forceinline__ void best_two(const float (&k)[V], float &a, float &b)
+{
+    a = k[0];
+    b = -__builtin_inff();
+#pragma unroll
+    for (int i = 1; i < V; ++i) {
+        b = __builtin_amdgcn_fmed3f(a, b, k[i]);   // of three in which a >= b
+        a = __builtin_elementwise_maximum(a, k[i]);
+    }
+}
+
+// The larger two of two pairs (a, b) and (c, d), each in order.
+__device__ __forceinline__ void merge_two(float &a, float &b, float c, float d)
+{
+    const float low = __builtin_elementwise_minimum(a, c);
+    a = __builtin_elementwise_maximum(a, c);
+    b = __builtin_elementwise_maximum(low, __builtin_elementwise_maximum(b, d));
+}
+
+// The best two keys of each lane's set of 2 * M lanes from those of its halves.
+template <int M>
+__device__ __forceinline__ void best_two_of(float &a, float &b)
+{
+    const Halves x = halves<M>(__float_as_uint(a)), y = halves<M>(__float_as_uint(b));
+    a = __uint_as_float(x.a);
+    b = __uint_as_float(y.a);
+    merge_two(a, b, __uint_as_float(x.b), __uint_as_float(y.b));
+}
+
+// 1 / (1 + exp(-x)) for V values, as sigmoid() rounds it.  The reciprocal's one
+// unit of error is taken out by a Newton step with fused multiply-adds, which
+// rounds correctly for every 1 <= d < 2^126; past that (x < -87.3) the quotient is
+// subnormal, and all V are divided.
+template <int V>
+__device__ __forceinline__ void sigmoids(const float (&x)[V], float (&s)[V])
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float d = 1.0f + expf(-x[i]), r = __builtin_amdgcn_rcpf(d);
+        s[i] = __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
+        most = __builtin_elementwise_maximum(most, d);
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // few registers, many waves
+    }
+    if (!(most < 0x1p126f))   // also for a NaN
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] = sigmoid(x[i]);
+}
+
+constexpr int kGathered = 16;   // keys the lanes of a row can place
+
+// LDS of one token.
+template <int LV, bool GROUPED>
+struct Scratch {
+    int id[XRED_MAX_TOPK];        // what was chosen, in order
+    float x[XRED_MAX_TOPK];
+    float best[16];
+    uint32_t gathered[kGathered];
+    int keys[GROUPED ? LV : 1];
+};
+
+// The topk rounds: each lane keeps the largest of its keys, and the lanes of a
+// token agree by a butterfly of maxima.
+template <int L, int V>
+__device__ __forceinline__ void choose_by_rounds(const float (&kf)[V], uint32_t topk, uint32_t lane,
+                                                 uint32_t first, int (&chosen)[XRED_MAX_TOPK])
+{
+    int key[V], own = kNone;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        key[i] = order_of(kf[i]);
+        own = key[i] > own ? key[i] : own;
+    }
+    for (uint32_t r = 0; r < topk; ++r) {
+        const int best = lanes_max<L>(own);
+        const bool any = best > kNegInf;
+        if (lowest_lane<L>(any && own == best, first) == lane) {
+            int id = 0;
+#pragma unroll
+            for (int i = V - 1; i >= 0; --i) id = key[i] == best ? i : id;
+            chosen[r] = (int)lane * V + id;
+            own = kNone;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                key[i] = i == id ? kNone : key[i];
+                own = key[i] > own ? key[i] : own;
+            }
+        }
+        if (!any && lane == 0) chosen[r] = -1;
+    }
+}
+
+// A bound that at least topk keys of the token reach, where there are as many: the
+// topk-th largest of 16 of its keys.  The lanes' best will do for a few slots.
+// For more, or where groups left out leave lanes without a key, these are the best
+// two of the 8 lanes with the largest best, which hold the largest keys but for a
+// third one in a lane; of 64 lanes, the best of the best four lanes in each row of
+// 16.  a, b: the lane's best two; topk at most 16.
+template <int L, int V, bool GROUPED>
+__device__ __forceinline__ float bound_of(float a, float b, uint32_t topk, uint32_t lane,
+                                          float (&best)[16])
+{
+    uint32_t place = place_in_row(order_of(a));
+    float v = a;
+    if (L == 64 || (V > 1 && (GROUPED || topk > 6))) {
+        if constexpr (L == 64) {
+            if (place < 4) best[lane / 16 * 4 + place] = a;
+        } else if (place < 8) {
+            best[place] = a;
+            best[8 + place] = b;
+        }
+        wave_sync();
+        v = best[lane % 16];
+        place = place_in_row(order_of(v));
+    }
+    return lanes_max<16>(place + 1 >= topk ? v : -__builtin_inff());
+}
+
+// Keys that are not among the group_topk best groups become -inf; a and b, the
+// lane's best two, follow.
+template <int L, int V>
+__device__ __forceinline__ void keep_groups(const RouteParams &p, float (&kf)[V], uint32_t lane,
+                                            uint32_t e0, uint32_t first, int (&row)[L * V],
+                                            float &a, float &b)
+{
+    uint64_t in;   // of a token's lanes
+    if (__builtin_amdgcn_ballot_w64(a != a) == 0 && p.group_lanes != 0) {
+        // groups are whole lanes, a power of two of them
+        float ga = a, gb = b;
+        if (p.group_lanes > 1) best_two_of<1>(ga, gb);
+        if (p.group_lanes > 2) best_two_of<2>(ga, gb);
+        if (p.group_lanes > 4) best_two_of<4>(ga, gb);
+        if (p.group_lanes > 8) best_two_of<8>(ga, gb);
+        if (L == 64 && p.group_lanes > 16) best_two_of<16>(ga, gb);
+        const uint32_t shift = 31 - __clz(p.group_lanes);
+        const bool head = (lane & (p.group_lanes - 1)) == 0 && e0 < p.experts;
+        int rank = head ? order_of(p.group_score == 2 && p.per_group > 1 ? ga + gb : ga) : kNone;
+        bool kept;
+        if constexpr (L == 16) {
+            // every lane takes part; an infinity less another (NaN) is first, and can
+            // be one place before the end of the integers
+            const uint32_t place = place_in_row(rank == INT32_MAX ? rank - 1 : rank);
+            kept = head && place < p.group_topk;
+        } else {
+            kept = false;
+            for (uint32_t r = 0; r < p.group_topk; ++r) {
+                const int best = lanes_max<L>(rank);
+                if (lowest_lane<L>(rank == best, first) == lane) {
+                    kept = true;
+                    rank = kNone;
+                }
+            }
+        }
+        in = __builtin_amdgcn_ballot_w64(kept) >> first;
+        const bool own = (in >> ((lane >> shift) << shift)) & 1;
+#pragma unroll
+        for (int i = 0; i < V; ++i) kf[i] = own ? kf[i] : -__builtin_inff();
+        a = own ? a : -__builtin_inff();
+        b = own ? b : -__builtin_inff();
+        return;
+    }
+    // any groups: every lane ranks one, from LDS
+#pragma unroll
+    for (int i = 0; i < V; ++i) row[e0 + i] = order_of(kf[i]);
+    wave_sync();
+    int rank = kNone;
+    if (lane < p.groups) {
+        int one = kNone, two = kNone;   // the best two
+        const uint32_t base = lane * p.per_group;
+        uint32_t at = lane % p.per_group;   // every lane from another bank
+        for (uint32_t i = 0; i < p.per_group; ++i) {
+            const int k = row[base + at];
+            at = at + 1 == p.per_group ? 0 : at + 1;
+            two = k > one ? one : k > two ? k : two;
+            one = k > one ? k : one;
+        }
+        rank = order_of(p.group_score == 2 && p.per_group > 1 ? value_of(one) + value_of(two)
+                                                              : value_of(one));
+    }
+    wave_sync();
+    bool kept = false;
+    for (uint32_t r = 0; r < p.group_topk; ++r) {
+        const int best = lanes_max<L>(rank);
+        if (lowest_lane<L>(rank == best, first) == lane) {
+            kept = true;
+            rank = kNone;
+        }
+    }
+    in = __builtin_amdgcn_ballot_w64(kept) >> first;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const uint32_t g = ((e0 + i) * p.per_group_inv) >> 20;
+        kf[i] = (in >> (g & 63)) & 1 ? kf[i] : -__builtin_inff();
+    }
+    best_two<V>(kf, a, b);
+}
+
 template <class T, int L, int V, bool SIGMOID, bool GROUPED>
 __global__ __launch_bounds__(64 * kWavesPerWg) void route_kernel(RouteParams p)
 {
-    constexpr int kTokens = 64 / L;                    // of a wave
-    constexpr int kSlots = (XRED_MAX_TOPK + L - 1) / L;   // chosen experts a lane finishes
-    __shared__ int chosen_id[kWavesPerWg][kTokens][XRED_MAX_TOPK];
-    __shared__ float chosen_x[kWavesPerWg][kTokens][XRED_MAX_TOPK];
-    __shared__ int keys[GROUPED ? kWavesPerWg : 1][GROUPED ? kTokens : 1][GROUPED ? L * V : 1];
+    constexpr int kTokens = 64 / L;   // of a wave
+    __shared__ Scratch<L * V, GROUPED> scratch[kWavesPerWg][kTokens];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t lane = threadIdx.x % L, seg = threadIdx.x % 64 / L, first = seg * L;
-    const uint32_t e0 = lane * V;
+    const bool all = p.experts == L * V;
+    auto &own = scratch[wave][seg];
     for (uint64_t t0 = ((uint64_t)blockIdx.x * kWavesPerWg + wave) * kTokens; t0 < p.tokens;
          t0 += (uint64_t)gridDim.x * kWavesPerWg * kTokens) {
         const bool live = t0 + seg < p.tokens;
         const uint64_t token = live ? t0 + seg : p.tokens - 1;
-        float x[V];
-        load_logits<T, V>(p.logits + token * p.stride, e0, p.experts, x);
-        int key[V];
+        const char *row = p.logits + token * p.stride;
+        // worked out anew for every token, or what only unusual rows need of it would
+        // be computed ahead of the loop
+        uint32_t e0 = lane * V;
+        __asm__ volatile("" : "+v"(e0));
+        float x[V], kf[V];
+        load_logits<T, V>(row, e0, p.experts, all, x);
+        if constexpr (SIGMOID) {
+            sigmoids<V>(x, kf);
+        } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float k = SIGMOID ? sigmoid(x[i]) : x[i];
-            if (p.bias && e0 + i < p.experts) k += p.bias[e0 + i];
-            key[i] = e0 + i >= p.experts ? kNone : x[i] == -__builtin_inff() ? kNegInf : order_of(k);
+            for (int i = 0; i < V; ++i) kf[i] = x[i];
         }
-        if constexpr (GROUPED) {
-            int(&row)[L * V] = keys[wave][seg];
+        if (p.bias) {
+            float b[V];
+            load_logits<TF32, V>((const char *)p.bias, e0, p.experts, all, b);
 #pragma unroll
-            for (int i = 0; i < V; ++i) row[e0 + i] = key[i];
-            wave_sync();
-            int rank = kNone;
-            if (lane < p.groups) {
-                int a = kNone, b = kNone;   // the best two
-                const uint32_t base = lane * p.per_group;
-                uint32_t at = lane % p.per_group;   // every lane from another bank
-                for (uint32_t i = 0; i < p.per_group; ++i) {
-                    const int k = row[base + at];
-                    at = at + 1 == p.per_group ? 0 : at + 1;
-                    b = k > a ? a : k > b ? k : b;
-                    a = k > a ? k : a;
-                }
-                rank = order_of(p.group_score == 2 && p.per_group > 1 ? value_of(a) + value_of(b)
-                                                                      : value_of(a));
-            }
-            wave_sync();
-            bool in = false;
-            for (uint32_t r = 0; r < p.group_topk; ++r) {
-                const int best = lanes_max<L>(rank);
-                if (lowest_lane<L>(rank == best, first) == lane) {
-                    in = true;
-                    rank = kNone;
-                }
-            }
-            const uint64_t groups = __builtin_amdgcn_ballot_w64(in) >> first;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const uint32_t g = ((e0 + i) * p.per_group_inv) >> 20;
-                if (!((groups >> (g & 63)) & 1)) key[i] = kNone;
-            }
+            for (int i = 0; i < V; ++i) kf[i] += b[i];
         }
-        int own = kNone;
+        if (SIGMOID || p.bias) {
+            float least = x[0];
 #pragma unroll
-        for (int i = 0; i < V; ++i) own = key[i] > own ? key[i] : own;
-        for (uint32_t r = 0; r < p.topk; ++r) {
-            const int best = lanes_max<L>(own);
-            const bool any = best > kNegInf;
-            const uint32_t from = lowest_lane<L>(any && own == best, first);
-            if (from == lane) {
-                int id = 0;
-                float cx = 0.0f;
+            for (int i = 1; i < V; ++i) least = __builtin_elementwise_minimum(least, x[i]);
+            if (!(least > -__builtin_inff()))   // also for a NaN
 #pragma unroll
-                for (int i = V - 1; i >= 0; --i)
-                    if (key[i] == best) {
-                        id = i;
-                        cx = x[i];
-                    }
-                chosen_id[wave][seg][r] = (int)e0 + id;
-                chosen_x[wave][seg][r] = cx;
-                own = kNone;
+                for (int i = 0; i < V; ++i) kf[i] = x[i] == -__builtin_inff() ? x[i] : kf[i];
+        }
+        float a, b;
+        best_two<V>(kf, a, b);
+        if constexpr (GROUPED) keep_groups<L, V>(p, kf, lane, e0, first, own.keys, a, b);
+
+        bool rounds = a != a || p.topk > kGathered;
+        uint32_t reach = 0, before = 0, count = 0;   // bit V - 1 - i: key i reaches the bound
+        if (__builtin_amdgcn_ballot_w64(rounds) == 0) {
+            float bound = bound_of<L, V, GROUPED>(a, b, p.topk, lane, own.best);
+            bound = bound > -__FLT_MAX__ ? bound : -__FLT_MAX__;   // -inf is not chosen
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    key[i] = i == id ? kNone : key[i];
-                    own = key[i] > own ? key[i] : own;
+            for (int i = 0; i < V; ++i) reach = reach + reach + (kf[i] >= bound ? 1 : 0);
+            lanes_before<L>(__popc(reach), before, count);
+            rounds = count > kGathered;
+        }
+        if (__builtin_amdgcn_ballot_w64(rounds) == 0) {
+            while (reach != 0) {
+                const uint32_t bit = 31 - __clz(reach);
+                own.gathered[before++] = e0 + V - 1 - bit;
+                reach ^= 1u << bit;
+            }
+            wave_sync();
+            // gathered in order of the experts, so place decides among equals
+            int key = kNone, e = 0;
+            float cx = 0.0f;
+            if (lane < count) {
+                e = (int)own.gathered[lane];
+                cx = up1<T>(row, e);
+                key = order_of((SIGMOID ? sigmoid(cx) : cx) + (p.bias ? p.bias[e] : 0.0f));
+            }
+            const uint32_t place = place_in_row(key);
+            if (lane < count) {
+                if (place < p.topk) {
+                    own.id[place] = e;
+                    own.x[place] = cx;
                 }
+            } else if (lane < p.topk) {
+                own.id[lane] = -1;
             }
-            if (!any && lane == 0) {
-                chosen_id[wave][seg][r] = -1;
-                chosen_x[wave][seg][r] = -__builtin_inff();
-            }
+        } else {
+            choose_by_rounds<L, V>(kf, p.topk, lane, first, own.id);
+            wave_sync();
+            for (uint32_t r = lane; r < p.topk; r += L)
+                if (own.id[r] >= 0) own.x[r] = up1<T>(row, own.id[r]);
         }
         wave_sync();
-        // weights: slot r of the token is finished by lane r % L
-        int id[kSlots];
-        float s[kSlots], total = 0.0f, top = -__builtin_inff();
-#pragma unroll
-        for (int q = 0; q < kSlots; ++q) {
-            const uint32_t r = q * L + lane;
-            id[q] = r < p.topk ? chosen_id[wave][seg][r] : -1;
-            s[q] = id[q] >= 0 ? chosen_x[wave][seg][r] : -__builtin_inff();
-            if (!SIGMOID) top = __builtin_elementwise_maximum(top, s[q]);
-        }
-        if constexpr (SIGMOID) {
-#pragma unroll
-            for (int q = 0; q < kSlots; ++q) {
-                s[q] = sigmoid(s[q]);
-                total += s[q];
-            }
-            if (p.renorm) total = lanes_sum<L>(total);
-            else total = 1.0f;
-        } else {
+        // weights: slot r of the token is finished by lane r % L, and every sum runs
+        // over the slots in one order, whichever way they were chosen
+        float total = 0.0f, top = -__builtin_inff();
+        auto value = [&](uint32_t r) {
+            return r < p.topk && own.id[r] >= 0 ? own.x[r] : -__builtin_inff();
+        };
+        if constexpr (!SIGMOID) {
+            for (uint32_t r = lane; r < p.topk; r += L)
+                top = __builtin_elementwise_maximum(top, value(r));
             if (!p.renorm)
 #pragma unroll
                 for (int i = 0; i < V; ++i) top = __builtin_elementwise_maximum(top, x[i]);
@@ -191,29 +415,31 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void route_kernel(RouteParams p)
 #pragma unroll
                 for (int i = 0; i < V; ++i) total += expf(x[i] - top);
             }
-#pragma unroll
-            for (int q = 0; q < kSlots; ++q) {
-                s[q] = expf(s[q] - top);
-                if (p.renorm) total += s[q];
-            }
-            total = lanes_sum<L>(total);
         }
-#pragma unroll
-        for (int q = 0; q < kSlots; ++q) {
-            const uint32_t r = q * L + lane;
-            if (live && r < p.topk) {
-                const float w = total == 0.0f ? 0.0f : s[q] / total;
-                p.ids[token * p.topk + r] = id[q];
-                p.weights[token * p.topk + r] = id[q] < 0 ? 0.0f : p.scale * w;
-            }
+        auto score = [&](float v) { return SIGMOID ? sigmoid(v) : expf(v - top); };
+        const float s = score(value(lane));   // of the lane's first slot
+        if (p.renorm) {
+            total = s;
+            for (uint32_t r = lane + L; r < p.topk; r += L) total += score(value(r));
         }
-        wave_sync();   // chosen_* are read before the next tokens' are written
+        total = p.renorm || !SIGMOID ? lanes_sum<L>(total) : 1.0f;
+        if (live)
+            for (uint32_t r = lane; r < p.topk; r += L) {
+                const int id = own.id[r];
+                const float v = r == lane ? s : score(value(r));
+                const float w = total == 0.0f ? 0.0f : v / total;
+                p.ids[token * p.topk + r] = id;
+                p.weights[token * p.topk + r] = id < 0 ? 0.0f : p.scale * w;
+            }
+        wave_sync();   // the scratch is read before the next tokens' is written
     }
 }
 
 template <class T, int L, int V>
-hipError_t go_route(const RouteParams &p, bool sigmoid, hipStream_t s)
+hipError_t go_route(RouteParams p, bool sigmoid, hipStream_t s)
 {
+    const uint32_t lanes = p.per_group / V;
+    p.group_lanes = p.per_group % V == 0 && (lanes & (lanes - 1)) == 0 && lanes < L ? lanes : 0;
     constexpr uint64_t per_wg = 64 / L * kWavesPerWg;
     const dim3 grid(grid_for((p.tokens + per_wg - 1) / per_wg)), block(64 * kWavesPerWg);
     if (p.groups > 1)
@@ -273,7 +499,7 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void route_grad_kernel(RouteGradP
         const uint64_t token = live ? t0 + seg : p.tokens - 1;
         const char *logits = p.logits + token * p.stride;
         float x[V];
-        if (dense) load_logits<T, V>(logits, e0, p.experts, x);
+        if (dense) load_logits<T, V>(logits, e0, p.experts, p.experts == L * V, x);
 #pragma unroll
         for (int i = 0; i < V; ++i) row[e0 + i] = 0.0f;
         uint32_t id[kSlots];
