@@ -15,9 +15,10 @@ namespace {
 // no atomic decides an order.
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kPlanSteps = 4;
 constexpr uint32_t kPlanTile = kPlanThreads * kPlanSteps;
-// Up to this many slots one workgroup plans alone (one launch); beyond, a first
-// launch counts, and each workgroup of the second adds up what lies before it.
-constexpr uint32_t kPlanAlone = 4 * kPlanTile;
+// Up to one tile a workgroup plans alone, in one launch (4096 slots 6.7 us); beyond,
+// a first launch counts, and each workgroup of the second adds up what lies before
+// it (16384 slots 8 us, where four tiles one after another took 20).
+constexpr uint32_t kPlanAlone = kPlanTile;
 constexpr uint32_t kPlanMostWgs = 128;
 
 struct PlanParams {
@@ -63,6 +64,21 @@ __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanParams p)
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     for (uint32_t b = blockIdx.x; b < p.wgs; b += gridDim.x) {
         const uint32_t lo = b * p.range, hi = p.n - lo < p.range ? p.n : lo + p.range;
+        // a tile's ids, on their way while the counts are added up or the tile before
+        // is written: its waves take as many steps as spread what is left over them all
+        uint32_t id[kPlanSteps];
+        auto steps_of = [&](uint32_t at) {
+            return hi - at >= kPlanTile ? (uint32_t)kPlanSteps
+                                        : (hi - at + kPlanThreads - 1) / kPlanThreads;
+        };
+        auto load_ids = [&](uint32_t at) {
+#pragma unroll
+            for (int s = 0; s < kPlanSteps; ++s) {
+                const uint32_t i = (wave * steps_of(at) + s) * 64 + lane;
+                id[s] = s < (int)steps_of(at) && i < hi - at ? (uint32_t)p.ids[at + i] : p.experts;
+            }
+        };
+        if (lo < hi) load_ids(lo);
         // counts of all slots, and of those before this range
         if (p.parts == nullptr) {
             plan_count(p, lo, hi, total);
@@ -76,7 +92,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanParams p)
             const uint32_t e = threadIdx.x % columns, share = kPlanThreads / columns;
             if (e < p.experts) {
                 uint32_t all = 0, before = 0;
-#pragma unroll 4
+#pragma unroll 8
                 for (uint32_t i = threadIdx.x / columns; i < p.wgs; i += share) {
                     const uint32_t c = p.parts[i * p.experts + e];
                     all += c;
@@ -90,16 +106,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanParams p)
         // offsets: an exclusive scan over the experts, one a thread
         static_assert(XRED_MAX_EXPERTS <= kPlanThreads, "one expert a thread");
         const uint32_t c = threadIdx.x < p.experts ? total[threadIdx.x] : 0;
-        uint32_t sum = c;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t x = __shfl_up(sum, d);
-            sum += (int)lane >= d ? x : 0;
-        }
-        if (lane == 63) wave_total[wave] = sum;
+        uint32_t first, all;
+        lanes_before<64>(c, first, all);
+        if (lane == 0) wave_total[wave] = all;
         __syncthreads();
-        uint32_t first = sum - c;
-        for (uint32_t w = 0; w < wave; ++w) first += wave_total[w];
+#pragma unroll
+        for (uint32_t w = 0; w < kPlanWaves; ++w) first += w < wave ? wave_total[w] : 0;
         if (threadIdx.x < p.experts) base[threadIdx.x] += first;
         if (b == 0 && threadIdx.x < p.experts) {
             p.counts[threadIdx.x] = (int32_t)c;
@@ -108,19 +120,13 @@ __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanParams p)
         }
         const uint32_t bits = 32 - __clz(p.experts);   // of an id, experts for "none" included
         for (uint32_t at = lo; at < hi; at += kPlanTile) {
-            const uint32_t left = hi - at;
-            // as many steps of a wave as spread what is left over all of them
-            const uint32_t steps = left >= kPlanTile ? kPlanSteps : (left + kPlanThreads - 1) / kPlanThreads;
+            const uint32_t left = hi - at, steps = steps_of(at);
             for (uint32_t e = lane; e < p.experts; e += 64) in_wave[wave][e] = 0;
-            uint32_t id[kPlanSteps], rank[kPlanSteps];
+            uint32_t rank[kPlanSteps];
             wave_sync();
 #pragma unroll
-            for (int s = 0; s < kPlanSteps; ++s) {
-                const uint32_t i = (wave * steps + s) * 64 + lane;
-                const bool on = s < (int)steps && i < left;
-                id[s] = on ? (uint32_t)p.ids[at + i] : p.experts;
-                if (id[s] > p.experts) id[s] = p.experts;
-            }
+            for (int s = 0; s < kPlanSteps; ++s)
+                if (id[s] > p.experts) id[s] = p.experts;   // no expert
 #pragma unroll
             for (int s = 0; s < kPlanSteps; ++s) {
                 rank[s] = 0;
@@ -146,12 +152,16 @@ __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanParams p)
             // each wave's first row of each expert, relative to base
             const uint32_t e = threadIdx.x;
             uint32_t tile = 0;
-            if (e < p.experts)
+            if (e < p.experts) {
+                uint32_t n[kPlanWaves];
+#pragma unroll
+                for (int w = 0; w < kPlanWaves; ++w) n[w] = in_wave[w][e];
+#pragma unroll
                 for (int w = 0; w < kPlanWaves; ++w) {
-                    const uint32_t x = in_wave[w][e];
                     in_wave[w][e] = (uint16_t)tile;
-                    tile += x;
+                    tile += n[w];
                 }
+            }
             __syncthreads();
 #pragma unroll
             for (int s = 0; s < kPlanSteps; ++s) {
@@ -165,6 +175,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanParams p)
             }
             __syncthreads();
             if (e < p.experts) base[e] += tile;
+            if (at + kPlanTile < hi) load_ids(at + kPlanTile);
         }
         __syncthreads();
     }

@@ -29,6 +29,7 @@ struct RouteParams {
     uint64_t tokens, stride;   // stride in bytes
     uint32_t experts, topk, groups, group_topk, group_score, per_group, per_group_inv;
     uint32_t group_lanes;   // lanes of a group, 0 unless whole ones and a power of two
+    uint32_t share;         // otherwise: lanes that rank a group, a power of two
     uint32_t renorm;
     float scale;
 };
@@ -95,23 +96,6 @@ __device__ __forceinline__ uint32_t place_in_row(int key, uint32_t rank = 0)
     } else {
         return rank;
     }
-}
-
-// Sum of x over the lanes below this one in its set of L, and over all of them.
-template <int L>
-__device__ __forceinline__ void lanes_before(uint32_t x, uint32_t &before, uint32_t &all)
-{
-    uint32_t s = x;   // row_shr 1, 2, 4, 8; then the rows before
-    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x111, 0xF, 0xF, true);
-    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x112, 0xF, 0xF, true);
-    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x114, 0xF, 0xF, true);
-    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x118, 0xF, 0xF, true);
-    if constexpr (L == 64) {
-        s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x142, 0xA, 0xF, false);
-        s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x143, 0xC, 0xF, false);
-    }
-    before = s - x;
-    all = (uint32_t)lanes_max<L>((int)s);
 }
 
 // The best two of V keys (-inf where there are fewer); a is NaN if one of them is.
@@ -234,6 +218,16 @@ __device__ __forceinline__ float bound_of(float a, float b, uint32_t topk, uint3
     return lanes_max<16>(place + 1 >= topk ? v : -__builtin_inff());
 }
 
+template <int M>
+__device__ __forceinline__ void best_two_of(int &a, int &b)
+{
+    const Halves x = halves<M>((uint32_t)a), y = halves<M>((uint32_t)b);
+    const int p = (int)x.a, q = (int)x.b, r = (int)y.a, t = (int)y.b;
+    const int low = p > q ? q : p, next = r > t ? r : t;
+    a = p > q ? p : q;
+    b = low > next ? low : next;
+}
+
 // Keys that are not among the group_topk best groups become -inf; a and b, the
 // lane's best two, follow.
 template <int L, int V>
@@ -277,24 +271,27 @@ __device__ __forceinline__ void keep_groups(const RouteParams &p, float (&kf)[V]
         b = own ? b : -__builtin_inff();
         return;
     }
-    // any groups: every lane ranks one, from LDS
+    // any groups, from LDS: p.share lanes look for one group's best two together
 #pragma unroll
     for (int i = 0; i < V; ++i) row[e0 + i] = order_of(kf[i]);
     wave_sync();
-    int rank = kNone;
-    if (lane < p.groups) {
-        int one = kNone, two = kNone;   // the best two
-        const uint32_t base = lane * p.per_group;
-        uint32_t at = lane % p.per_group;   // every lane from another bank
-        for (uint32_t i = 0; i < p.per_group; ++i) {
-            const int k = row[base + at];
-            at = at + 1 == p.per_group ? 0 : at + 1;
+    const uint32_t g = lane / p.share, base = g * p.per_group;
+    int one = kNone, two = kNone;   // in order
+    if (g < p.groups)
+        for (uint32_t i = lane % p.share; i < p.per_group; i += p.share) {
+            const int k = row[base + i];
             two = k > one ? one : k > two ? k : two;
             one = k > one ? k : one;
         }
-        rank = order_of(p.group_score == 2 && p.per_group > 1 ? value_of(one) + value_of(two)
-                                                              : value_of(one));
-    }
+    if (p.share > 1) best_two_of<1>(one, two);
+    if (p.share > 2) best_two_of<2>(one, two);
+    if (p.share > 4) best_two_of<4>(one, two);
+    if (L == 64 && p.share > 8) best_two_of<8>(one, two);
+    if (L == 64 && p.share > 16) best_two_of<16>(one, two);
+    const bool head = g < p.groups && lane % p.share == 0;
+    const float sum = p.group_score == 2 && p.per_group > 1 ? value_of(one) + value_of(two)
+                                                            : value_of(one);
+    int rank = head ? order_of(sum) : kNone;
     wave_sync();
     bool kept = false;
     for (uint32_t r = 0; r < p.group_topk; ++r) {
@@ -307,8 +304,8 @@ __device__ __forceinline__ void keep_groups(const RouteParams &p, float (&kf)[V]
     in = __builtin_amdgcn_ballot_w64(kept) >> first;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const uint32_t g = ((e0 + i) * p.per_group_inv) >> 20;
-        kf[i] = (in >> (g & 63)) & 1 ? kf[i] : -__builtin_inff();
+        const uint32_t at = (((e0 + i) * p.per_group_inv) >> 20) * p.share;   // its group's lane
+        kf[i] = (in >> (at & 63)) & 1 ? kf[i] : -__builtin_inff();
     }
     best_two<V>(kf, a, b);
 }
@@ -440,6 +437,7 @@ hipError_t go_route(RouteParams p, bool sigmoid, hipStream_t s)
 {
     const uint32_t lanes = p.per_group / V;
     p.group_lanes = p.per_group % V == 0 && (lanes & (lanes - 1)) == 0 && lanes < L ? lanes : 0;
+    for (p.share = 1; 2 * p.share * p.groups <= L;) p.share *= 2;
     constexpr uint64_t per_wg = 64 / L * kWavesPerWg;
     const dim3 grid(grid_for((p.tokens + per_wg - 1) / per_wg)), block(64 * kWavesPerWg);
     if (p.groups > 1)

@@ -193,6 +193,23 @@ __device__ __forceinline__ int lanes_max(int x)
     }
 }
 
+// Sum of x over the lanes below this one in its set of L, and over all of them.
+template <int L>
+__device__ __forceinline__ void lanes_before(uint32_t x, uint32_t &before, uint32_t &all)
+{
+    uint32_t s = x;   // row_shr 1, 2, 4, 8; then the rows before
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x111, 0xF, 0xF, true);
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x112, 0xF, 0xF, true);
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x114, 0xF, 0xF, true);
+    s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x118, 0xF, 0xF, true);
+    if constexpr (L == 64) {
+        s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x142, 0xA, 0xF, false);
+        s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x143, 0xC, 0xF, false);
+    }
+    before = s - x;
+    all = (uint32_t)lanes_max<L>((int)s);
+}
+
 // Orders a wave's LDS accesses before it against those after it, for lanes that
 // read what other lanes of their wave wrote.
 __device__ __forceinline__ void wave_sync()

@@ -12,6 +12,7 @@
 // argument is kept, no result of a check is remembered.
 #include <Python.h>
 
+#include <ATen/Functions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
 
@@ -455,12 +456,20 @@ xred_score score_of(PyObject *o)
     throw Decline{};
 }
 
-// The caller's workspace; a call that needs one but was given none is left to
-// the Python code, which allocates it.
-void *workspace_of(PyObject *o, c10::Device dev, uint64_t need, uint64_t *bytes)
+// The caller's workspace, or one from torch's allocator into `keep`, which belongs
+// to the current stream; on a stream that the caller names the Python code
+// allocates it.
+void *workspace_of(PyObject *o, c10::Device dev, uint64_t need, PyObject *stream,
+                   uint64_t *bytes, at::Tensor *keep)
 {
     *bytes = 0;
     if (need == 0) return nullptr;
+    if (o == Py_None) {
+        if (stream != Py_None) throw Decline{};
+        *keep = at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(dev));
+        *bytes = need;
+        return keep->data_ptr();
+    }
     const at::Tensor &t = tensor(o);
     if (!t.is_cuda() || t.device() != dev || !t.is_contiguous()) throw Decline{};
     *bytes = (uint64_t)t.numel() * t.element_size();
@@ -522,7 +531,8 @@ PyObject *fold_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         n.rstd = (const float *)vector(a[2], m.dev, m.rows, at::kFloat);
         n.dweight = (float *)vector(a[6], m.dev, m.columns, at::kFloat);
         const uint64_t need = n.dweight ? f_fold_norm_grad_workspace(n.rows, n.hidden) : 0;
-        n.workspace = workspace_of(a[7], m.dev, need, &n.workspace_bytes);
+        at::Tensor keep;
+        n.workspace = workspace_of(a[7], m.dev, need, a[8], &n.workspace_bytes, &keep);
         void *stream = stream_of(a[8], m.dev);
         return unlocked([&] { return f_fold_norm_grad(&n, stream); });
     });
@@ -595,9 +605,10 @@ PyObject *dispatch_plan(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         n.offsets = (int32_t *)vector(a[2], dev, experts + 1, at::kInt);
         n.pos = (int32_t *)slots(a[3], dev, tokens, k, at::kInt);
         n.slots = (int32_t *)vector(a[4], dev, tokens * k, at::kInt);
+        at::Tensor keep;
         n.workspace = workspace_of(a[5], dev,
                                    f_dispatch_plan_workspace((uint64_t)(tokens * k), n.experts),
-                                   &n.workspace_bytes);
+                                   a[6], &n.workspace_bytes, &keep);
         void *stream = stream_of(a[6], dev);
         return unlocked([&] { return f_dispatch_plan(&n, stream); });
     });

@@ -150,13 +150,12 @@ def fold_norm_grad(dout, sum, rstd, dx, *, weight=None, dsum=None, dweight=None,
     the residual and of every source, and dweight (fp32).  dsum: the gradient
     that reaches fold_norm's sum; workspace: a tensor to use for dweight's
     partial sums instead of one from torch's allocator."""
-    if dweight is not None and workspace is None:
-        workspace = _workspace(load().xred_fold_norm_grad_workspace(*_shape(sum, "sum")), sum,
-                               stream)
     st = native().fold_norm_grad(dout, sum, rstd, dx, weight, dsum, dweight, workspace, stream)
     if st is not None:   # plain tensors; anything else is checked below
         return check(st)
     rows, hidden = _shape(sum, "sum")
+    if dweight is not None and workspace is None:
+        workspace = _workspace(load().xred_fold_norm_grad_workspace(rows, hidden), sum, stream)
     dt, dev = _dtype_name(sum, None), sum.device
     es = ELEM_SIZE[dt]
     for what, t in (("dout", dout), ("dsum", dsum), ("dx", dx)):
@@ -230,15 +229,14 @@ def dispatch_plan(ids, counts, offsets, pos, *, slots=None, workspace=None, stre
     experts; offsets: experts + 1; pos: tokens x topk, each slot's row or -1;
     slots (optional, tokens * topk): each row's slot.  workspace: a tensor to use
     instead of one from torch's allocator."""
-    if workspace is None:
-        tokens, topk = _shape(ids, "ids")
-        need = load().xred_dispatch_plan_workspace(tokens * topk, counts.numel())
-        workspace = _workspace(need, ids, stream) if need else None
     st = native().dispatch_plan(ids, counts, offsets, pos, slots, workspace, stream)
     if st is not None:   # plain tensors; anything else is checked below
         return check(st)
     tokens, topk = _shape(ids, "ids")
     experts, dev = counts.numel(), ids.device
+    need = load().xred_dispatch_plan_workspace(tokens * topk, experts)
+    if need and workspace is None:
+        workspace = _workspace(need, ids, stream)
     a = DispatchPlanArgs(
         tokens, experts, topk, _slots(ids, tokens, topk, "ids", dev, ("i32",)),
         _ints(counts, experts, "counts", dev), _ints(offsets, experts + 1, "offsets", dev),

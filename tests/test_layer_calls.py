@@ -190,7 +190,7 @@ def test_nothing_to_do_succeeds(L):
 def test_workspace_sizes(L):
     assert L.xred_fold_norm_grad_workspace(0, 64) == 0
     for r in (1, 255, 256, 4096, 1 << 20):
-        assert 0 < L.xred_fold_norm_grad_workspace(r, 100) <= min(r, 1024) * 400
+        assert 0 < L.xred_fold_norm_grad_workspace(r, 100) <= min(r, 12 * 256) * 400
     assert L.xred_dispatch_plan_workspace(1, 64) == 0
     assert 0 < L.xred_dispatch_plan_workspace(2 ** 31 - 1, 1024) <= 1 << 20
 
