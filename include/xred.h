@@ -641,7 +641,8 @@ XRED_API xred_status xred_combine_grad(const xred_combine_grad_args *args, void 
 
 /*
  * CU budget: at most max_workgroups workgroups per launch of the fused,
- * reduce-scatter, step-wise, cast and batched kernels (0 = no limit, the
+ * reduce-scatter, step-wise, cast and batched kernels and of those of the calls
+ * around a reduced activation (0 = no limit, the
  * default), so a reduction can run beside compute kernels on the rest of the
  * chip -- the paper's FTAR kernel uses two thread blocks and stays hidden
  * behind the network (Section 5).  Results do not depend on it.  Process-wide;
