@@ -13,7 +13,7 @@
 // (a NaN, more than 16 keys that reach the bound) take the rounds.
 //
 // 65536 tokens x 256 experts fp32, sigmoid, 8 groups, top 8: 37.5 us (1.9 TB/s of
-// logits; by rounds 74 us), some 1350 vector instructions for a wave's 4 tokens, of
+// logits; by rounds 74 us), some 1170 vector instructions for a wave's 4 tokens, of
 // which the sigmoids are a quarter; softmax over 65536 x 256 bf16 18 us; 4 tokens
 // 4.3 us.  The gradient is bound by HBM and the launch: 32768 x 128 bf16 with every
 // logit's 6.8 us, 2.7 TB/s.  (Hardware exponentials for a first choice, with the exact
