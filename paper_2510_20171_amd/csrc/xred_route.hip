@@ -482,7 +482,7 @@ struct RouteGradParams {
 
 // With s the scores of the chosen, S their sum, dw = scale * dweights:
 //   sigmoid          dx_j = dw_j s_j (1 - s_j)
-//   sigmoid, renorm  dx_j = (dw_j - sum_i dw_i s_i / S) / S * s_j (1 - s_j)
+//   sigmoid, renorm  dx_j = (dw_j - sum_i dw_i s_i / S) * s_j / S * (1 - s_j)
 //   softmax, renorm  dx_j = p_j (dw_j - sum_i dw_i p_i), p the softmax of the chosen
 //   softmax          dx_e = p_e (dw_e - sum_i dw_i p_i) for every expert e, dw_e 0
 //                    where e is not chosen
@@ -546,34 +546,37 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void route_grad_kernel(RouteGradP
 #pragma unroll
             for (int i = 0; i < V; ++i) x[i] = (x[i] * inv) * (g[i] - mean);
         } else {
+            float rest[kSlots], mean = 0.0f;   // 1 - s, of which 1 less s would leave little
             if constexpr (SIGMOID) {
 #pragma unroll
                 for (int q = 0; q < kSlots; ++q) {
+                    rest[q] = sigmoid(-s[q]);
                     s[q] = sigmoid(s[q]);
                     total += s[q];
-                    dot += d[q] * s[q];
                 }
             } else {
                 top = lanes_max<L>(top);
                 const float shift = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
                 for (int q = 0; q < kSlots; ++q) {
+                    rest[q] = 1.0f;
                     s[q] = expf(s[q] - shift);
                     total += s[q];
-                    dot += d[q] * s[q];
                 }
             }
-            float inv = 1.0f, mean = 0.0f;
             if (p.renorm) {
+                // parts of the sum, which may be subnormal: its reciprocal overflows
                 total = lanes_sum<L>(total);
-                dot = lanes_sum<L>(dot);
-                inv = total == 0.0f ? 0.0f : 1.0f / total;
-                mean = dot * inv;
+#pragma unroll
+                for (int q = 0; q < kSlots; ++q) {
+                    s[q] = total == 0.0f ? 0.0f : s[q] / total;
+                    dot += d[q] * s[q];
+                }
+                mean = lanes_sum<L>(dot);
             }
 #pragma unroll
             for (int q = 0; q < kSlots; ++q)
-                if (id[q] < p.experts)
-                    row[id[q]] = ((d[q] - mean) * inv) * (SIGMOID ? s[q] * (1.0f - s[q]) : s[q]);
+                if (id[q] < p.experts) row[id[q]] = (d[q] - mean) * s[q] * rest[q];
             wave_sync();
 #pragma unroll
             for (int i = 0; i < V; ++i) x[i] = row[e0 + i];

@@ -250,6 +250,36 @@ def test_gradient_against_the_formula(xr, dtype, experts):
                 near(wide[:, :experts], want, err + 2.0 ** -126, (score, renorm, tokens))
 
 
+@pytest.mark.parametrize("low,high", [(-88.6, -86.0), (-40.0, -20.0), (5.0, 30.0)])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_gradient_of_a_saturated_sigmoid(xr, low, high, renorm):
+    """Scores that are subnormal, or that leave 1 - s far below s's unit: each element is
+    good to a part of itself.  r bounds a score's and its complement's own error: half a
+    subnormal unit (2^-150, doubled for the product it comes from) and some units of
+    2^-24 for the exponential, the sum and the quotient.  The quotient by the scores' sum
+    doubles it, the mean it enters doubles that, and D bounds |dweights * scale|."""
+    g = gen(11)
+    t, e, k = 33, 40, 8
+    x = low + (high - low) * torch.rand(t, e, generator=g, device="cuda")
+    dw = randn(g, t, k)
+    ids = torch.empty((t, k), dtype=torch.int32, device="cuda")
+    w, dx = torch.empty((t, k), device="cuda"), torch.empty_like(x)
+    xr.route(x, ids, w, score="sigmoid", renorm=renorm, scale=1.5)
+    xr.route_grad(x, ids, dw, dx, score="sigmoid", renorm=renorm, scale=1.5)
+    at = ids.long()
+    v = x.double().gather(1, at)
+    s, rest = torch.sigmoid(v), torch.sigmoid(-v)
+    d = 1.5 * dw.double()
+    r = 2.0 ** -149 / s.amin(1, True) + 2.0 ** -20
+    if renorm:
+        s = s / s.sum(1, True)
+        d = d - (d * s).sum(1, True)
+    want = torch.zeros(t, e, dtype=torch.float64, device="cuda").scatter(1, at, d * s * rest)
+    most = 1.5 * dw.double().abs().amax(1, True)
+    err = torch.zeros_like(want).scatter(1, at, 8 * r * most * s * rest + 2.0 ** -148)
+    assert bool(((dx.double() - want).abs() <= err).all())
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("renorm", [False, True])
 def test_gradient_against_differences(xr, score, renorm):
