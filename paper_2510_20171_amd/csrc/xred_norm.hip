@@ -3,18 +3,19 @@
 //
 // The row's mean of squares needs the whole row before any element of y can be
 // written, so a row stays in registers between the two: the threads of a
-// workgroup (of a wave, for rows of up to 64 pieces) hold V pieces each, and HBM
-// sees every input and output once.  The row scale of an 8-bit output is
+// workgroup (rows of up to 64 pieces: 8, 16, 32 or 64 lanes) hold V pieces each, and
+// HBM sees every input and output once.  The row scale of an 8-bit output is
 // rstd * max |h * weight|, so it comes out of the same reduction.
 //
-// Bound by HBM from some hundred rows on: 8192 x 4096 bf16, 8 sources, residual,
-// sum, bf16 and 8-bit outputs 129 us, 6.0 TB/s (a kernel that only moves 9 such
-// streams in and 2.5 out: 6.4); one source with an 8-bit output 47 us, 5.0 TB/s;
-// 1999 x 5003 fp16, two sources 22 us, 4.5 TB/s, from the 256 MB cache.  The
-// gradient of 16384 x 4096 bf16 90 us, 5.9 TB/s (3 streams in, 1 out: 6.4).  One row
-// takes 4.3 us, most of it the launch.  (Keeping the next row's loads in flight
-// while one is worked on made the gradient slower, 96 us at best: a wait for loads
-// also waits for the stores before them.)
+// Bound by HBM from some hundred rows on: 8192 x 4096 bf16, 8 sources, residual, sum,
+// bf16 and 8-bit outputs 129 us, 6.0 TB/s (a kernel that only moves 9 such streams in
+// and 2.5 out: 6.4); one source with an 8-bit output 47 us, 5.0 TB/s; 131072 x 128
+// bf16, one source, residual and sum 25 us (a wave a row: 71); 1999 x 5003 fp16, two
+// sources 22 us, 4.5 TB/s, from the 256 MB cache.  The gradient of 16384 x 4096 bf16 90
+// us, 5.9 TB/s (3 streams in, 1 out: 6.4).  One row takes 4.3 us, most of it the
+// launch.  (Keeping the next row's loads in flight while one is worked on made the
+// gradient slower, 96 us at best: a wait for loads also waits for the stores before
+// them.)
 #include "xred_layer.hpp"
 #include "xred_rows.hpp"
 
@@ -24,7 +25,8 @@ namespace {
 // Sources folded into registers, at most this many 16-byte loads of them in
 // flight a lane (with the residual's and the weight's).
 constexpr int kInFlight = 8;
-constexpr int kRowsPerWg = 4;   // where a wave holds a row
+constexpr int kWaves = 4;   // of a workgroup in which L lanes hold a row
+constexpr int rows_per_wg(int l) { return l ? kWaves * 64 / l : 1; }
 
 // The source pointers, by value (a type of its own: an expression of the header's
 // unnamed enum in a kernel's parameters gives it other names on host and device).
@@ -87,16 +89,17 @@ __device__ __forceinline__ void narrow()
     if constexpr (is_wide<T, V>()) __builtin_amdgcn_sched_barrier(0);
 }
 
-// Sum, and with MAX a maximum of magnitudes, over the waves of a row.  WG: the
-// workgroup's waves share the row; red then holds 2 * kMostWaves floats, and a
-// barrier has to come between two uses of it.
+// Sum, and on demand a maximum of magnitudes, over the L lanes that hold a row, or
+// (L 0) over the workgroup; red then holds 2 * kMostWaves floats, and a barrier has
+// to come between two uses of it.
 constexpr int kMostWaves = 16;
-template <bool WG>
+template <int L>
 __device__ __forceinline__ void row_reduce(float &s, float &m, bool max, float *red)
 {
-    s = lanes_sum<64>(s);
-    if (max) m = lanes_max<64>(m);
-    if constexpr (WG) {
+    constexpr int kLanes = L ? L : 64;
+    s = lanes_sum<kLanes>(s);
+    if (max) m = lanes_max<kLanes>(m);
+    if constexpr (L == 0) {
         const uint32_t wave = threadIdx.x / 64, waves = blockDim.x / 64;
         if (threadIdx.x % 64 == 0) {
             red[wave] = s;
@@ -109,15 +112,26 @@ __device__ __forceinline__ void row_reduce(float &s, float &m, bool max, float *
     }
 }
 
-// The largest |y| of each lane's group of `lanes` lanes.
+// The largest |y| of each lane's group of `lanes` lanes, at most MOST.
+template <uint32_t MOST>
 __device__ __forceinline__ float group_max(float m, uint32_t lanes)
 {
     m = lanes_max<4>(m);   // the smallest group: 32 elements of 8 a lane
     if (lanes >= 8) m = lanes_max<8, 4>(m);
-    if (lanes >= 16) m = lanes_max<16, 8>(m);
-    if (lanes >= 32) m = lanes_max<32, 16>(m);
-    if (lanes >= 64) m = lanes_max<64, 32>(m);
+    if (MOST >= 16 && lanes >= 16) m = lanes_max<16, 8>(m);
+    if (MOST >= 32 && lanes >= 32) m = lanes_max<32, 16>(m);
+    if (MOST >= 64 && lanes >= 64) m = lanes_max<64, 32>(m);
     return m;
+}
+
+// Which of a workgroup's rows this thread works on.
+template <int L>
+__device__ __forceinline__ uint32_t row_of()
+{
+    if constexpr (L == 0) return 0;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if constexpr (L == 64) return wave;   // the same in all lanes: scalar addresses
+    else return wave * (64 / L) + threadIdx.x % 64 / L;
 }
 
 // 1 / 448 and 1 / scale are good to a unit in the last place, far inside e4m3's
@@ -128,22 +142,22 @@ __device__ __forceinline__ float e4m3_scale(float amax)
     return __builtin_elementwise_maximum(amax, 0x1p-100f) * (1.0f / 448.0f);
 }
 
-// NP: the number of sources, 0: any (p.nsrc).  V pieces a thread; a row belongs
-// to a workgroup of at most THREADS threads, or (THREADS 0) to a wave.
-template <class T, int NP, int V, int THREADS>
-__global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm_kernel(
-    NormParams p, NormSources<NP> src)
+// NP: the number of sources, 0: any (p.nsrc).  V pieces a thread; a row belongs to
+// L lanes, or (L 0) to a workgroup of at most 1024 threads.
+template <class T, int NP, int V, int L>
+__global__ __launch_bounds__(L ? 64 * kWaves : 1024) void fold_norm_kernel(NormParams p,
+                                                                          NormSources<NP> src)
 {
-    constexpr bool kWg = THREADS != 0;
-    constexpr int RPB = kWg ? 1 : kRowsPerWg;
+    constexpr bool kWg = L == 0, WIDE = is_wide<T, V>();
+    constexpr int RPB = rows_per_wg(L);
     constexpr int N = T::kVec;
-    constexpr int G = NP != 0 ? NP : V >= kInFlight ? 1 : kInFlight / V;
+    constexpr int G = NP != 0 ? NP : WIDE ? 1 : kInFlight / V;
     // groups of 512 elements of fp32 lie in two waves (go_norm sees to it that each
     // pair is whole); a row's reduction comes between two uses of `pair`
     constexpr bool kPairs = kWg && N == 4;
     __shared__ float red[2][2 * kMostWaves], pair[kPairs ? V : 1][kPairs ? kMostWaves : 1];
-    const uint32_t TPR = kWg ? blockDim.x : 64, tid = kWg ? threadIdx.x : threadIdx.x % 64;
-    const uint32_t sub = kWg ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t TPR = kWg ? blockDim.x : L, tid = kWg ? threadIdx.x : threadIdx.x % TPR;
+    const uint32_t sub = row_of<L>();
     const uint32_t nsrc = NP ? NP : p.nsrc;
     uint32_t c[V], from[V];
 #pragma unroll
@@ -152,8 +166,11 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
         from[v] = piece_from<N>(v * TPR + tid, c[v], p.hidden) * T::kSize;
     }
     int turn = 0;
-    for (uint64_t row = (uint64_t)blockIdx.x * RPB + sub; row < p.rows;
-         row += (uint64_t)gridDim.x * RPB) {
+    for (uint64_t row0 = (uint64_t)blockIdx.x * RPB; row0 < p.rows;
+         row0 += (uint64_t)gridDim.x * RPB) {
+        // past the last row lanes go along on it and store nothing
+        const bool live = kWg || row0 + sub < p.rows;
+        const uint64_t row = live ? row0 + sub : p.rows - 1;
         float h[V][N];
         const uint64_t at = row * p.src_stride;
         const char *res = p.residual ? p.residual + row * p.residual_stride : nullptr;
@@ -179,7 +196,7 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
                         }
             };
             u32x4 r[V];
-            if (res)
+            if (res && !WIDE)
 #pragma unroll
                 for (int v = 0; v < V; ++v) r[v] = load_piece(res, from[v]);
             if constexpr (NP != 0) fold(0);
@@ -188,11 +205,12 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
             for (int v = 0; v < V; ++v) {
                 if (res) {
                     float x[N];
-                    up_vec<T>(r[v], x);
+                    up_vec<T>(WIDE ? load_piece(res, from[v]) : r[v], x);
 #pragma unroll
                     for (int j = 0; j < N; ++j) h[v][j] += x[j];
                 }
                 settle<N>(h[v], c[v], p.hidden);
+                narrow<T, V>();
             }
         } else {
 #pragma unroll
@@ -222,16 +240,16 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
                 narrow<T, V>();
             }
         }
-        row_reduce<kWg>(s, m, row_scale, red[turn]);
+        row_reduce<L>(s, m, row_scale, red[turn]);
         turn ^= 1;   // the next row's reduction leaves this one's values alone
         const float rstd = rsqrtf(s * p.inv_hidden + p.eps);
-        if (p.rstd && tid == 0) p.rstd[row] = rstd;
+        if (p.rstd && tid == 0 && live) p.rstd[row] = rstd;
         const float row_amax = m * rstd;
-        if (row_scale && tid == 0) p.scale[row * p.scale_stride] = e4m3_scale(row_amax);
+        if (row_scale && tid == 0 && live) p.scale[row * p.scale_stride] = e4m3_scale(row_amax);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t piece = v * TPR + tid, off = piece * 16;
-            if (p.sum) store_piece<T>(p.sum + row * p.sum_stride, off, c[v], h[v]);
+            const uint32_t piece = v * TPR + tid, off = piece * 16, there = live ? c[v] : 0;
+            if (p.sum) store_piece<T>(p.sum + row * p.sum_stride, off, there, h[v]);
             float w[N];
             weight_piece<T>(p.weight, p.wide_weight, piece, c[v], p.hidden, w);
             float a = 0.0f;
@@ -240,9 +258,10 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
                 h[v][j] = h[v][j] * (rstd * w[j]);   // one rounding of what may be subnormal
                 a = __builtin_elementwise_maximum(a, __builtin_fabsf(h[v][j]));
             }
-            if (p.out) store_piece<T>(p.out + row * p.out_stride, off, c[v], h[v]);
+            if (p.out) store_piece<T>(p.out + row * p.out_stride, off, there, h[v]);
             if (p.out8) {
-                if (p.group) a = group_max(a, p.group / N < 64 ? p.group / N : 64);
+                constexpr uint32_t kMost = L ? L : 64;
+                if (p.group) a = group_max<kMost>(a, p.group / N < kMost ? p.group / N : kMost);
                 if constexpr (kPairs)
                     if (p.group / N == 128) {   // a pair of waves
                         if (tid % 64 == 0) pair[v][tid / 64] = a;
@@ -250,7 +269,7 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
                         a = __builtin_elementwise_maximum(a, pair[v][tid / 64 ^ 1]);
                     }
                 const float scale = e4m3_scale(p.group ? a : row_amax);
-                if (p.group && c[v] != 0 && piece % (p.group / N) == 0)
+                if (p.group && there != 0 && piece % (p.group / N) == 0)
                     p.scale[row * p.scale_stride + piece / (p.group / N)] = scale;
                 const float inv = __builtin_amdgcn_rcpf(scale);
                 float y[N];
@@ -261,23 +280,23 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void fold_norm
                 if (p.group == 0)
 #pragma unroll
                     for (int j = 0; j < N; ++j) y[j] = e4m3_clamp(y[j]);
-                store_piece_e4m3<N>(p.out8 + row * p.out8_stride, piece * N, c[v], y);
+                store_piece_e4m3<N>(p.out8 + row * p.out8_stride, piece * N, there, y);
             }
             narrow<T, V>();
         }
     }
 }
 
-template <class T, int NP, int V, int THREADS>
+template <class T, int NP, int V, int L>
 hipError_t go_norm(const NormParams &p, const void *const *srcs, unsigned threads, hipStream_t s)
 {
     NormSources<NP> src{};
     for (uint32_t i = 0; i < p.nsrc; ++i) src.p[i] = (const char *)srcs[i];
-    const unsigned rows = THREADS ? 1 : kRowsPerWg;
+    const unsigned rows = rows_per_wg(L);
     if (T::kVec == 4 && p.group == 512) threads = (threads + 127) / 128 * 128;
-    return launch_kernel(fold_norm_kernel<T, NP, V, THREADS>,
+    return launch_kernel(fold_norm_kernel<T, NP, V, L>,
                          dim3(grid_for((p.rows + rows - 1) / rows)),
-                         dim3(THREADS ? threads : 64 * kRowsPerWg), 0, s, p, src);
+                         dim3(L ? 64 * kWaves : threads), 0, s, p, src);
 }
 
 // Threads for `pieces` pieces of a row, V each, in whole waves.
@@ -286,17 +305,23 @@ unsigned row_threads(uint32_t pieces, uint32_t v) { return (pieces + 64 * v - 1)
 // One piece a thread, so that a row's loads are all on their way at once; two
 // where few sources would leave a thread few loads, and there are rows enough to
 // fill the chip all the same (8192 x 4096 bf16, one source, 8-bit output: 47 us
-// against 51; 1999 x 5003 fp16, two sources 22 / 24; eight sources 134 / 130).
+// against 51; 1999 x 5003 fp16, two sources 22 / 24; eight sources 134 / 130).  Few
+// sources: up to four, whose number the kernel knows (8192 x 5120 bf16, three: 82 us,
+// with the kernel for any number 120; eight are alike).  Short rows share a wave.
 template <class T, int NP>
 hipError_t go_norm_shape(const NormParams &p, const void *const *srcs, hipStream_t s)
 {
     const uint32_t pieces = (p.hidden + T::kVec - 1) / T::kVec;
-    if (pieces <= 64) return go_norm<T, NP, 1, 0>(p, srcs, 64, s);
+    constexpr int ANY = NP == 1 ? 1 : 0;
+    if (pieces <= 8) return go_norm<T, ANY, 1, 8>(p, srcs, 0, s);
+    if (pieces <= 16) return go_norm<T, ANY, 1, 16>(p, srcs, 0, s);
+    if (pieces <= 32) return go_norm<T, ANY, 1, 32>(p, srcs, 0, s);
+    if (pieces <= 64) return go_norm<T, NP, 1, 64>(p, srcs, 0, s);
     const bool two = NP != 0 && pieces > 128 && p.rows > 2 * (uint64_t)device_cus();
-    if (pieces <= 1024 && !two) return go_norm<T, NP, 1, 1024>(p, srcs, row_threads(pieces, 1), s);
-    if (pieces <= 2048) return go_norm<T, NP, 2, 1024>(p, srcs, row_threads(pieces, 2), s);
-    if (pieces <= 4096) return go_norm<T, 0, 4, 1024>(p, srcs, row_threads(pieces, 4), s);
-    if constexpr (T::kVec == 4) return go_norm<T, 0, 8, 1024>(p, srcs, row_threads(pieces, 8), s);
+    if (pieces <= 1024 && !two) return go_norm<T, NP, 1, 0>(p, srcs, row_threads(pieces, 1), s);
+    if (pieces <= 2048) return go_norm<T, NP, 2, 0>(p, srcs, row_threads(pieces, 2), s);
+    if (pieces <= 4096) return go_norm<T, 0, 4, 0>(p, srcs, row_threads(pieces, 4), s);
+    if constexpr (T::kVec == 4) return go_norm<T, 0, 8, 0>(p, srcs, row_threads(pieces, 8), s);
     return hipErrorInvalidValue;
 }
 static_assert(XRED_MAX_HIDDEN <= 1024 * 32, "the widest row is 32 elements a thread");
@@ -314,18 +339,18 @@ struct NormGradParams {
 };
 
 // dweight sums over rows, dx over a row: the threads that hold a row keep their
-// columns' part of dweight in registers over all rows of a slice (rows slice,
-// slice + slices, ...), so both come from one pass over dout and sum.  LEAN: rows
-// too wide for dsum and the weight to wait in registers too.
-template <class T, int V, int THREADS>
-__global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad_kernel(
-    NormGradParams p)
+// columns' part of dweight in registers over all rows of a slice (the workgroup's
+// rows at slice, slice + slices, ...), so both come from one pass over dout and sum.
+// LEAN: rows too wide to wait in registers are read again, from the cache.
+template <class T, int V, int L, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradParams p)
 {
-    constexpr bool kWg = THREADS != 0, LEAN = is_wide<T, V>();
-    constexpr int N = T::kVec, RPB = kWg ? 1 : kRowsPerWg;
+    constexpr bool kWg = L == 0, LEAN = is_wide<T, V>();
+    constexpr int N = T::kVec, RPB = rows_per_wg(L);
     __shared__ float red[2][2 * kMostWaves];
-    const uint32_t TPR = kWg ? blockDim.x : 64, tid = kWg ? threadIdx.x : threadIdx.x % 64;
-    const uint32_t sub = kWg ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    __shared__ float join[kWg ? 1 : RPB][kWg ? 1 : L * V * N];
+    const uint32_t TPR = kWg ? blockDim.x : L, tid = kWg ? threadIdx.x : threadIdx.x % TPR;
+    const uint32_t sub = row_of<L>();
     uint32_t c[V], from[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -333,12 +358,12 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad
         from[v] = piece_from<N>(v * TPR + tid, c[v], p.hidden) * T::kSize;
     }
     // a piece that was loaded, in place; rows shorter than one are read here
-    auto up = [&](u32x4 in, const char *row, int v, float(&x)[N]) {
+    auto up = [&](u32x4 in, const char *row, int v, uint32_t there, float(&x)[N]) {
         if (p.hidden >= N) {
             up_vec<T>(in, x);
-            settle<N>(x, c[v], p.hidden);
+            settle<N>(x, there, p.hidden);
         } else {
-            up_short<T>(row, c[v], x);
+            up_short<T>(row, there, x);
         }
     };
     auto load = [&](const char *row, int v) {
@@ -354,68 +379,77 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad
 #pragma unroll
         for (int v = 0; v < V; ++v) weights(v);
     int turn = 0;
-    for (uint32_t slice = blockIdx.x * RPB + sub; slice < p.slices; slice += gridDim.x * RPB) {
+    for (uint32_t slice = blockIdx.x; slice < p.slices; slice += gridDim.x) {
         float dw[V][N];
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int j = 0; j < N; ++j) dw[v][j] = 0.0f;
-        for (uint64_t row = slice; row < p.rows; row += p.slices) {
+        for (uint64_t row0 = (uint64_t)slice * RPB; row0 < p.rows;
+             row0 += (uint64_t)p.slices * RPB) {
+            // past the last row lanes go along on it, as if it had no elements
+            const bool live = kWg || row0 + sub < p.rows;
+            const uint64_t row = live ? row0 + sub : p.rows - 1;
             const float rstd = p.rstd[row];
             const char *dout = p.dout + row * p.dout_stride, *sum = p.sum + row * p.sum_stride;
             const char *dsum = p.dsum ? p.dsum + row * p.dsum_stride : nullptr;
             u32x4 a[V], b[V], d[V];
+            if (!LEAN)
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                a[v] = load(dout, v);
-                b[v] = load(sum, v);
-                if (!LEAN && dsum) d[v] = load(dsum, v);
-            }
+                for (int v = 0; v < V; ++v) {
+                    a[v] = load(dout, v);
+                    b[v] = load(sum, v);
+                    if (dsum) d[v] = load(dsum, v);
+                }
             float s = 0.0f, unused = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float g[N], n[N];
-                up(a[v], dout, v, g);
-                up(b[v], sum, v, n);
+                const uint32_t there = live ? c[v] : 0;
+                up(LEAN ? load(dout, v) : a[v], dout, v, there, g);
+                up(LEAN ? load(sum, v) : b[v], sum, v, there, n);
                 if (LEAN) weights(v);
-                narrow<T, V>();
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     n[j] *= rstd;
                     dw[v][j] = __builtin_fmaf(g[j], n[j], dw[v][j]);
                     s = __builtin_fmaf(g[j] * w[v][j], n[j], s);
                 }
+                narrow<T, V>();
             }
             // converted again below: kept in 32 bits across the reduction, the
             // pieces would take twice the registers
+            if (!LEAN)
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                opaque_piece(a[v]);
-                opaque_piece(b[v]);
-            }
-            row_reduce<kWg>(s, unused, false, red[turn]);
+                for (int v = 0; v < V; ++v) {
+                    opaque_piece(a[v]);
+                    opaque_piece(b[v]);
+                }
+            row_reduce<L>(s, unused, false, red[turn]);
             turn ^= 1;
             const float mean = s * p.inv_hidden;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float g[N], n[N];
-                up(a[v], dout, v, g);
-                up(b[v], sum, v, n);
+                const uint32_t there = live ? c[v] : 0;
+                up(LEAN ? load(dout, v) : a[v], dout, v, there, g);
+                up(LEAN ? load(sum, v) : b[v], sum, v, there, n);
                 if (LEAN) weights(v);
 #pragma unroll
                 for (int j = 0; j < N; ++j)
                     g[j] = rstd * (g[j] * w[v][j] - (n[j] * rstd) * mean);
                 if (dsum) {
-                    up(LEAN ? load(dsum, v) : d[v], dsum, v, n);
+                    up(LEAN ? load(dsum, v) : d[v], dsum, v, there, n);
 #pragma unroll
                     for (int j = 0; j < N; ++j) g[j] += n[j];
                 }
-                store_piece<T>(p.dx + row * p.dx_stride, (v * TPR + tid) * 16, c[v], g);
+                store_piece<T>(p.dx + row * p.dx_stride, (v * TPR + tid) * 16, there, g);
                 narrow<T, V>();
             }
         }
-        if (p.partial) {
-            char *part = (char *)(p.partial + (uint64_t)slice * p.hidden);
+        if (p.partial == nullptr) continue;
+        float *part = p.partial + (uint64_t)slice * p.hidden;
+        if constexpr (kWg) {
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -423,8 +457,22 @@ __global__ __launch_bounds__(THREADS ? THREADS : 64 * kRowsPerWg) void norm_grad
                     const uint32_t at = (v * TPR + tid) * N + 4 * k;
                     const float four[4] = {dw[v][4 * k], dw[v][4 * k + 1], dw[v][4 * k + 2],
                                            dw[v][4 * k + 3]};
-                    store_piece<TF32>(part, at * 4, piece_count<4>(at / 4, p.hidden), four);
+                    store_piece<TF32>((char *)part, at * 4, piece_count<4>(at / 4, p.hidden), four);
                 }
+        } else {
+            // the workgroup's rows in order
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int j = 0; j < N; ++j) join[sub][(v * L + tid) * N + j] = dw[v][j];
+            __syncthreads();
+            for (uint32_t col = threadIdx.x; col < p.hidden; col += THREADS) {
+                float s = join[0][col];
+#pragma unroll
+                for (int r = 1; r < RPB; ++r) s += join[r][col];
+                part[col] = s;
+            }
+            __syncthreads();
         }
     }
 }
@@ -455,16 +503,20 @@ __global__ __launch_bounds__(kJoinColumns *kJoinParts) void norm_dweight_kernel(
     }
 }
 
-template <class T, int V, int THREADS>
+template <class T, int V, int L, int THREADS>
 hipError_t go_grad(const NormGradParams &p, unsigned threads, hipStream_t s)
 {
-    const unsigned slices = THREADS ? 1 : kRowsPerWg;
-    return launch_kernel(norm_grad_kernel<T, V, THREADS>,
-                         dim3(grid_for((p.slices + slices - 1) / slices)),
-                         dim3(THREADS ? threads : 64 * kRowsPerWg), 0, s, p);
+    return launch_kernel(norm_grad_kernel<T, V, L, THREADS>, dim3(grid_for(p.slices)),
+                         dim3(threads), 0, s, p);
 }
 
-// Pieces a thread of a row's workgroup, for rows past a wave.
+// Lanes that hold a short row, up to 8 elements each, or 0.
+int grad_lanes(uint64_t hidden)
+{
+    return hidden <= 64 ? 8 : hidden <= 128 ? 16 : hidden <= 256 ? 32 : hidden <= 512 ? 64 : 0;
+}
+
+// Pieces a thread of a longer row's workgroup.
 uint32_t grad_pieces(uint32_t pieces)
 {
     return pieces <= 512 ? 1 : pieces <= 2048 ? 2 : pieces <= 4096 ? 4 : 8;
@@ -473,14 +525,20 @@ uint32_t grad_pieces(uint32_t pieces)
 template <class T>
 hipError_t go_grad_shape(const NormGradParams &p, hipStream_t s)
 {
+    constexpr int V = 8 / T::kVec, SHORT = 64 * kWaves;
+    switch (grad_lanes(p.hidden)) {
+    case 8: return go_grad<T, V, 8, SHORT>(p, SHORT, s);
+    case 16: return go_grad<T, V, 16, SHORT>(p, SHORT, s);
+    case 32: return go_grad<T, V, 32, SHORT>(p, SHORT, s);
+    case 64: return go_grad<T, V, 64, SHORT>(p, SHORT, s);
+    }
     const uint32_t pieces = (p.hidden + T::kVec - 1) / T::kVec;
-    if (pieces <= 64) return go_grad<T, 1, 0>(p, 64, s);
     const uint32_t v = grad_pieces(pieces);
     const unsigned threads = row_threads(pieces, v);
-    if (v == 1) return go_grad<T, 1, 512>(p, threads, s);
-    if (v == 2) return go_grad<T, 2, 1024>(p, threads, s);
-    if (v == 4) return go_grad<T, 4, 1024>(p, threads, s);
-    if constexpr (T::kVec == 4) return go_grad<T, 8, 1024>(p, threads, s);
+    if (v == 1) return go_grad<T, 1, 0, 512>(p, threads, s);
+    if (v == 2) return go_grad<T, 2, 0, 1024>(p, threads, s);
+    if (v == 4) return go_grad<T, 4, 0, 1024>(p, threads, s);
+    if constexpr (T::kVec == 4) return go_grad<T, 8, 0, 1024>(p, threads, s);
     return hipErrorInvalidValue;
 }
 
@@ -489,15 +547,18 @@ hipError_t go_grad_shape(const NormGradParams &p, hipStream_t s)
 // As many slices as put 12 waves on each CU, where HBM delivers the most beside
 // three streams that are read (16384 x 4096 bf16, 8 / 12 / 16 / 24 waves: 112 / 90 /
 // 94 / 104 us), but at least 8 rows a slice, which keeps the partial sums' traffic
-// small beside the rows'.  (Counted for 2-byte types; rows of fp32 take up to
-// twice the waves.)
+// small beside the rows'.  (Counted for 2-byte types; long rows of fp32 take up to
+// twice the waves.)  Short rows: the waves of a workgroup join their sums in LDS, a
+// quarter of the parts or fewer (65536 x 512 bf16: 48 us, a part a wave 63).
 uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden)
 {
+    const int lanes = grad_lanes(hidden);
     const uint32_t pieces = (uint32_t)((hidden + 7) / 8);
-    const uint64_t waves = row_threads(pieces, grad_pieces(pieces)) / 64;
+    const uint64_t waves = lanes ? kWaves : row_threads(pieces, grad_pieces(pieces)) / 64;
     const uint64_t fill = 12 * 256 / (waves ? waves : 1), share = rows / 8 > 256 ? rows / 8 : 256;
-    const uint64_t s = fill < share ? fill : share;
-    return (uint32_t)(rows < s ? rows : s);
+    const uint64_t s = fill < share ? fill : share, per = rows_per_wg(lanes);
+    const uint64_t most = (rows + per - 1) / per;
+    return (uint32_t)(most < s ? most : s);
 }
 
 hipError_t launch_fold_norm(const xred_fold_norm_args &a, hipStream_t stream)
@@ -528,6 +589,8 @@ hipError_t launch_fold_norm(const xred_fold_norm_args &a, hipStream_t stream)
         using T = decltype(t);
         if (a.nsrc == 1) return go_norm_shape<T, 1>(p, a.srcs, stream);
         if (a.nsrc == 2) return go_norm_shape<T, 2>(p, a.srcs, stream);
+        if (a.nsrc == 3) return go_norm_shape<T, 3>(p, a.srcs, stream);
+        if (a.nsrc == 4) return go_norm_shape<T, 4>(p, a.srcs, stream);
         return go_norm_shape<T, 0>(p, a.srcs, stream);
     });
 }

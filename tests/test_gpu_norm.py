@@ -160,6 +160,19 @@ def test_many_rows(xr):
         run(xr, srcs, srcs[0], 1 + randn(g, hidden, scale=0.1).bfloat16(), 32)
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("hidden", [15, 32, 61, 64, 65, 100, 128, 129, 250, 256, 257, 500, 512])
+def test_short_rows(xr, dtype, hidden):
+    """Several rows a wave, numbers of rows that leave some of its lanes without one."""
+    g = gen(hidden + 1)
+    dt = DT[dtype]
+    for k, rows in enumerate((1, 2, 5, 31, 32, 33, 127, 130)):
+        srcs = [randn(g, rows, hidden).to(dt) for _ in range((1, 2, 5, 4)[k % 4])]
+        res = view(randn(g, rows, hidden).to(dt), 1, 1)[0] if k % 3 else None
+        w = (1 + randn(g, hidden, scale=0.3)).to(dt) if k % 2 else None
+        run(xr, srcs, res, w, (32, 128, 512, 0, 64, 256, 128, -1)[k], out=k != 2, pad=k % 5)
+
+
 def test_special_values(xr):
     """Zero rows, infinities and NaN stay in their rows; subnormal and huge rows."""
     g = gen(9)
@@ -228,6 +241,25 @@ def test_gradient_against_the_formula(xr, dtype, rows, hidden):
         over = dout.contiguous()
         xr.fold_norm_grad(over, h, rstd, over, weight=w, dsum=dsum)
         assert torch.equal(over, dx)
+
+
+@pytest.mark.parametrize("hidden", [9, 64, 100, 128, 200, 256, 512])
+@pytest.mark.parametrize("rows", [1, 15, 33, 4099, 30001])
+def test_gradient_of_short_rows(xr, rows, hidden):
+    """A column of ones for g and n = +-1 by turns: dweight counts rows exactly, and
+    dx = rstd (g - n mean(g n)) is +-1 or 0 by the row's own balance."""
+    for dt in DT.values():
+        sign = torch.ones(rows, hidden, device="cuda")
+        sign[1::2] = -1
+        d = torch.ones(rows, hidden, device="cuda").to(dt)
+        rstd = torch.ones(rows, device="cuda")
+        dw = torch.empty(hidden, device="cuda")
+        wide = torch.full((rows, hidden + 3), 7.0, device="cuda").to(dt)
+        xr.fold_norm_grad(d, sign.to(dt), rstd, wide[:, :hidden], dweight=dw)
+        assert bool((wide[:, hidden:] == 7).all())
+        assert bool((dw == rows % 2).all())
+        # mean(g n) n = 1 up to 1 / hidden's rounding, a part of 2^-24, and the sum's
+        assert bool((wide[:, :hidden].float().abs() <= hidden * 2.0 ** -24 + 2.0 ** -23).all())
 
 
 def test_gradient_against_differences(xr):
