@@ -172,7 +172,9 @@ XRED_API xred_status xred_fold_norm(const xred_fold_norm_args *args, void *hip_s
 
 XRED_API size_t xred_fold_norm_grad_workspace(uint64_t rows, uint64_t hidden)
 {
-    return hidden > XRED_MAX_HIDDEN ? 0 : (size_t)norm_grad_slices(rows, hidden) * hidden * 4;
+    if (hidden > XRED_MAX_HIDDEN) return 0;
+    const uint32_t a = norm_grad_slices(rows, hidden, 2), b = norm_grad_slices(rows, hidden, 4);
+    return (size_t)(a > b ? a : b) * hidden * 4;
 }
 
 XRED_API xred_status xred_fold_norm_grad(const xred_fold_norm_grad_args *args, void *hip_stream)

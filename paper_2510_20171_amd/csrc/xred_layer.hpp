@@ -10,7 +10,7 @@ namespace xred {
 
 hipError_t launch_fold_norm(const xred_fold_norm_args &a, hipStream_t stream);
 // Rows of the gradient's partial sums of dweight.
-uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden);
+uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden, uint64_t elem_size);
 hipError_t launch_fold_norm_grad(const xred_fold_norm_grad_args &a, hipStream_t stream);
 
 hipError_t launch_route(const xred_route_args &a, hipStream_t stream);

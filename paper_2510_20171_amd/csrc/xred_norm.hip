@@ -477,9 +477,9 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradParams p)
     }
 }
 
-// dweight[i] = the slices' parts, added in an order that their number fixes: 16
-// threads a column take every 16th slice each, then join.
-constexpr int kJoinColumns = 64, kJoinParts = 16;
+// dweight[i] = the slices' parts, added in an order that their number fixes: 32
+// threads a column take every 32nd slice each, then join.
+constexpr int kJoinColumns = 32, kJoinParts = 32;
 __global__ __launch_bounds__(kJoinColumns *kJoinParts) void norm_dweight_kernel(
     const float *partial, float *dweight, uint32_t hidden, uint32_t slices)
 {
@@ -544,20 +544,21 @@ hipError_t go_grad_shape(const NormGradParams &p, hipStream_t s)
 
 }  // namespace
 
-// As many slices as put 12 waves on each CU, where HBM delivers the most beside
-// three streams that are read (16384 x 4096 bf16, 8 / 12 / 16 / 24 waves: 112 / 90 /
-// 94 / 104 us), but at least 8 rows a slice, which keeps the partial sums' traffic
-// small beside the rows'.  (Counted for 2-byte types; long rows of fp32 take up to
-// twice the waves.)  Short rows: the waves of a workgroup join their sums in LDS, a
-// quarter of the parts or fewer (65536 x 512 bf16: 48 us, a part a wave 63).
-uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden)
+// As many slices as put some 12 waves on each CU, where HBM delivers the most beside
+// three streams that are read (16384 x 4096 bf16, 8 / 12 / 16 / 24 waves: 111 / 90 / 93 /
+// 102 us), in whole workgroups where few make them up (8192 x 5120 bf16, 512 / 614 / 768
+// workgroups of 5 waves: 61 / 86 / 74 us), but at least 8 rows a slice, which keeps the
+// partial sums' traffic small beside the rows'.  Short rows: the waves of a workgroup
+// join their sums in LDS, a quarter of the parts or fewer (65536 x 512 bf16: 48 us, a
+// part a wave 63).
+uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden, uint64_t es)
 {
     const int lanes = grad_lanes(hidden);
-    const uint32_t pieces = (uint32_t)((hidden + 7) / 8);
-    const uint64_t waves = lanes ? kWaves : row_threads(pieces, grad_pieces(pieces)) / 64;
-    const uint64_t fill = 12 * 256 / (waves ? waves : 1), share = rows / 8 > 256 ? rows / 8 : 256;
-    const uint64_t s = fill < share ? fill : share, per = rows_per_wg(lanes);
-    const uint64_t most = (rows + per - 1) / per;
+    const uint32_t pieces = (uint32_t)((hidden * es + 15) / 16), v = grad_pieces(pieces);
+    const uint32_t waves = lanes || hidden == 0 ? kWaves : row_threads(pieces, v) / 64;
+    const uint64_t fill = waves >= 12 ? 256 : waves > 8 || v > 1 ? 512 : 24 / waves * 128;
+    const uint64_t share = rows / 8 > 256 ? rows / 8 : 256, s = fill < share ? fill : share;
+    const uint64_t per = rows_per_wg(lanes), most = (rows + per - 1) / per;
     return (uint32_t)(most < s ? most : s);
 }
 
@@ -613,7 +614,7 @@ hipError_t launch_fold_norm_grad(const xred_fold_norm_grad_args &a, hipStream_t 
     p.dx_stride = a.dx.stride * es;
     p.hidden = (uint32_t)a.hidden;
     p.inv_hidden = 1.0f / (float)a.hidden;
-    p.slices = norm_grad_slices(a.rows, a.hidden);
+    p.slices = norm_grad_slices(a.rows, a.hidden, es);
     p.wide_weight = a.weight_dtype == XRED_FLOAT32;
     if (a.rows) {
         const hipError_t e = with_dtype_among<TF32, TBF16, TF16>(

@@ -73,7 +73,7 @@ GRAD = dict(rows=4, hidden=64, dout=rows(0), sum=rows(1), dsum=rows(2), dx=rows(
 GRAD_BAD = [
     (dict(dtype=3), UNSUPPORTED), (dict(hidden=32769), UNSUPPORTED), (dict(dout=NONE), INVALID),
     (dict(sum=NONE), INVALID), (dict(rstd=None), INVALID), (dict(dx=NONE), INVALID),
-    (dict(workspace=None), INVALID), (dict(workspace_bytes=1023), INVALID),
+    (dict(workspace=None), INVALID), (dict(workspace_bytes=255), INVALID),
     (dict(workspace=at(7, 8)), INVALID), (dict(weight_dtype=2), UNSUPPORTED),
     (dict(dx=rows(1)), ALIAS), (dict(dx=rows(0, 64, 2)), ALIAS), (dict(dweight=at(4)), ALIAS),
     (dict(workspace=at(6)), ALIAS), (dict(workspace=at(0)), ALIAS), (dict(dsum=rows(2, 10)), INVALID),
