@@ -547,8 +547,9 @@ hipError_t go_grad_shape(const NormGradParams &p, hipStream_t s)
 // As many slices as put some 12 waves on each CU, where HBM delivers the most beside
 // three streams that are read (16384 x 4096 bf16, 8 / 12 / 16 / 24 waves: 111 / 90 / 93 /
 // 102 us), in whole workgroups where few make them up (8192 x 5120 bf16, 512 / 614 / 768
-// workgroups of 5 waves: 61 / 86 / 74 us), but at least 8 rows a slice, which keeps the
-// partial sums' traffic small beside the rows'.  Short rows: the waves of a workgroup
+// workgroups of 5 waves: 61 / 86 / 74 us), but at least 4 rows a slice, which keeps the
+// partial sums' traffic below the rows' (2048 x 768, 2 / 4 / 8 rows: 11.7 / 12.2 / 15.8 us;
+// 1024 x 8192: 23.1 / 21.4 / 21.5).  Short rows: the waves of a workgroup
 // join their sums in LDS, a quarter of the parts or fewer (65536 x 512 bf16: 48 us, a
 // part a wave 63).
 uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden, uint64_t es)
@@ -557,9 +558,9 @@ uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden, uint64_t es)
     const uint32_t pieces = (uint32_t)((hidden * es + 15) / 16), v = grad_pieces(pieces);
     const uint32_t waves = lanes || hidden == 0 ? kWaves : row_threads(pieces, v) / 64;
     const uint64_t fill = waves >= 12 ? 256 : waves > 8 || v > 1 ? 512 : 24 / waves * 128;
-    const uint64_t share = rows / 8 > 256 ? rows / 8 : 256, s = fill < share ? fill : share;
-    const uint64_t per = rows_per_wg(lanes), most = (rows + per - 1) / per;
-    return (uint32_t)(most < s ? most : s);
+    const uint64_t per = rows_per_wg(lanes), one = (rows + per - 1) / per, four = rows / 4;
+    const uint64_t most = lanes || one < 256 ? one : four > 256 ? four : 256;
+    return (uint32_t)(most < fill ? most : fill);
 }
 
 hipError_t launch_fold_norm(const xred_fold_norm_args &a, hipStream_t stream)
