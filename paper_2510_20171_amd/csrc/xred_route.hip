@@ -507,7 +507,7 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void route_grad_kernel(RouteGradP
         float x[V];
         if (dense) load_logits<T, V>(logits, e0, p.experts, p.experts == L * V, x);
 #pragma unroll
-        for (int i = 0; i < V; ++i) row[e0 + i] = 0.0f;
+        for (int i = 0; i < V; ++i) row[(i / 4 * L + lane) * 4 + i % 4] = 0.0f;
         uint32_t id[kSlots];
         float d[kSlots], s[kSlots], top = -__builtin_inff();
 #pragma unroll
@@ -544,7 +544,7 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void route_grad_kernel(RouteGradP
             const float inv = total == 0.0f ? 0.0f : 1.0f / total;
             const float mean = dot * inv;
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = (x[i] * inv) * (g[i] - mean);
+            for (int i = 0; i < V; ++i) row[e0 + i] = (x[i] * inv) * (g[i] - mean);
         } else {
             float rest[kSlots], mean = 0.0f;   // 1 - s, of which 1 less s would leave little
             if constexpr (SIGMOID) {
@@ -577,33 +577,31 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void route_grad_kernel(RouteGradP
 #pragma unroll
             for (int q = 0; q < kSlots; ++q)
                 if (id[q] < p.experts) row[id[q]] = (d[q] - mean) * s[q] * rest[q];
-            wave_sync();
+        }
+        wave_sync();
+        if (live) {
+            // neighbouring lanes write neighbouring pieces
+            constexpr int N = T::kVec;
+            char *out = p.dlogits + token * p.dstride;
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = row[e0 + i];
+            for (int i = 0; i < (L * V / N + L - 1) / L; ++i) {
+                const uint32_t piece = i * L + lane, e = piece * N;
+                const uint32_t c = piece_count<N>(piece, p.experts);
+                if (c == 0) continue;
+                float a[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) a[j] = row[e + j];
+                if (c == N)
+                    __builtin_nontemporal_store(
+                        down_vec<T, OpSum>(a),
+                        (__attribute__((address_space(1))) u32x4_any *)((global_out)out + 16 * piece));
+                else
+#pragma unroll
+                    for (uint32_t j = 0; j < N; ++j)
+                        if (j < c) down1<T, OpSum>(out, e + j, a[j]);
+            }
         }
         wave_sync();   // the row is read before the next tokens' is written
-        if (live) {
-            char *out = p.dlogits + token * p.dstride;
-            bool done = false;
-            if constexpr (V % T::kVec == 0) {
-                if (e0 + V <= p.experts) {
-                    done = true;
-#pragma unroll
-                    for (int i = 0; i < V / T::kVec; ++i) {
-                        float a[T::kVec];
-#pragma unroll
-                        for (int j = 0; j < T::kVec; ++j) a[j] = x[i * T::kVec + j];
-                        *(__attribute__((address_space(1))) u32x4_any *)((global_out)out +
-                                                                         e0 * T::kSize + 16 * i) =
-                            down_vec<T, OpSum>(a);
-                    }
-                }
-            }
-            if (!done)
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (e0 + i < p.experts) down1<T, OpSum>(out, e0 + i, x[i]);
-        }
     }
 }
 
