@@ -184,6 +184,27 @@ def test_strides(xr):
         check(xr, wide[::2, lo:lo + e], 6, score="softmax", renorm=False)
 
 
+@pytest.mark.parametrize("experts,groups", [(129, 1), (160, 8), (160, 5), (200, 1), (256, 1), (256, 8),
+                                            (256, 16), (256, 32), (255, 5)])
+@pytest.mark.parametrize("tokens", [40, 2111])
+def test_few_and_many_tokens(xr, tokens, experts, groups):
+    """Either number of lanes a token, with masks, ties and infinities among the rows."""
+    g = gen(tokens + experts + groups)
+    x = randn(g, tokens, experts)
+    x[::5] = x[::5].round()                                     # ties
+    x[torch.rand(tokens, experts, generator=g, device="cuda") < 0.2] = -math.inf
+    x[7] = -math.inf
+    x[11, 1:] = -math.inf
+    x[13, 3] = math.nan
+    x[17, :9] = torch.finfo(torch.float32).min
+    x[23, 5] = math.inf
+    bias = randn(g, experts, scale=0.1)
+    for k in (1, 6, 8, 10, 16, 20):
+        for score, b in (("sigmoid", bias), ("softmax", None)):
+            check(xr, x, k, score=score, bias=b, groups=groups, group_topk=(groups + 1) // 2,
+                  renorm=k != 6)
+
+
 def test_many_tokens(xr):
     g = gen(6)
     check(xr, randn(g, 70003, 64).bfloat16(), 6, score="softmax", renorm=False)
