@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanParams p)
             __syncthreads();
             // every thread an expert and some of the workgroups: a column of
             // `parts` is short, and its loads would wait for one another
-            const uint32_t columns = p.experts <= 64 ? 64 : p.experts <= 256 ? 256 : kPlanThreads;
+            const uint32_t columns = p.experts <= 64 ? 64 : 1u << (32 - __clz(p.experts - 1));
             const uint32_t e = threadIdx.x % columns, share = kPlanThreads / columns;
             if (e < p.experts) {
                 uint32_t all = 0, before = 0;
