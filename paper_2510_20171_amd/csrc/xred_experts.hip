@@ -487,7 +487,13 @@ hipError_t go_combine_grad(const CombineGradParams &p, hipStream_t s)
         return launch_kernel(combine_grad_kernel<T, SLOTS, 0>,
                              dim3(grid_for((p.tokens + kItemWaves - 1) / kItemWaves)),
                              dim3(64 * kItemWaves), 0, s, p);
-    const uint32_t threads = pieces >= 1024 ? 1024 : (pieces + 63) / 64 * 64;
+    // one pass where a thread has several slots' loads; with one or two slots smaller
+    // workgroups, more of them at different stages (16384 x 4096 bf16, one slot: 65 us
+    // with 256 threads, 91 with 512; fp32 124 and 214; but 4 slots 60 and 52, and 64
+    // tokens with one slot 4.9 and 4.3)
+    const uint32_t most = p.topk <= 2 && p.tokens > 2 * (uint64_t)device_cus() ? 256 : 1024;
+    const uint32_t passes = (pieces + most - 1) / most;
+    const uint32_t threads = ((pieces + passes - 1) / passes + 63) / 64 * 64;
     return launch_kernel(combine_grad_kernel<T, SLOTS, 1024>, dim3(grid_for(p.tokens)),
                          dim3(threads), 0, s, p);
 }
