@@ -16,7 +16,7 @@
 // logits; by rounds 74 us), some 1170 vector instructions for a wave's 4 tokens, of
 // which the sigmoids are a quarter; softmax over 65536 x 256 bf16 18 us; 4 tokens
 // 4.3 us.  The gradient is bound by HBM and the launch: 32768 x 128 bf16 with every
-// logit's 6.8 us, 2.7 TB/s.  (Hardware exponentials for a first choice, with the exact
+// logit's 6.3 us, 2.9 TB/s.  (Hardware exponentials for a first choice, with the exact
 // keys computed for what it gathers, save a sixth of the instructions but took twice
 // the registers, 57 us.)
 #include "xred_layer.hpp"
