@@ -83,15 +83,17 @@ def _weight(t, dtype, n, device):
 
 
 def _workspace(nbytes, like, stream):
-    """A workspace from torch's allocator, which knows it by the stream of the call."""
+    """A workspace from torch's allocator, taken on the stream of the call: kernels
+    enqueued before on the stream it is taken on may still use the block, and only
+    that stream's later work waits for them."""
     import torch
-    t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-    if stream is not None:   # else it belongs to the stream the call runs on
-        if not isinstance(stream, torch.cuda.Stream):
-            handle = int(getattr(stream, "cuda_stream", stream))
-            stream = torch.cuda.ExternalStream(handle, device=like.device)
-        t.record_stream(stream)
-    return t
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = int(getattr(stream, "cuda_stream", stream))
+        stream = torch.cuda.ExternalStream(handle, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
 
 
 def _given(t, device):
