@@ -485,7 +485,7 @@ hipError_t go_combine_grad(const CombineGradParams &p, hipStream_t s)
     // against 36 with two waves a row)
     if (pieces <= 128)
         return launch_kernel(combine_grad_kernel<T, SLOTS, 0>,
-                             dim3(grid_for((p.tokens + kItemWaves - 1) / kItemWaves)),
+                             dim3(grid_of((p.tokens + kItemWaves - 1) / kItemWaves, 64 * kItemWaves)),
                              dim3(64 * kItemWaves), 0, s, p);
     // one pass where a thread has several slots' loads; with one or two slots smaller
     // workgroups, more of them at different stages (16384 x 4096 bf16, one slot: 65 us
@@ -494,7 +494,7 @@ hipError_t go_combine_grad(const CombineGradParams &p, hipStream_t s)
     const uint32_t most = p.topk <= 2 && p.tokens > 2 * (uint64_t)device_cus() ? 256 : 1024;
     const uint32_t passes = (pieces + most - 1) / most;
     const uint32_t threads = ((pieces + passes - 1) / passes + 63) / 64 * 64;
-    return launch_kernel(combine_grad_kernel<T, SLOTS, 1024>, dim3(grid_for(p.tokens)),
+    return launch_kernel(combine_grad_kernel<T, SLOTS, 1024>, dim3(grid_of(p.tokens, threads)),
                          dim3(threads), 0, s, p);
 }
 

@@ -8,6 +8,14 @@
 
 namespace xred {
 
+// Workgroups of `threads` threads for `wgs` parts of the work, which a workgroup takes
+// gridDim.x apart: a launch has to have fewer than 2^32 threads.
+inline unsigned grid_of(uint64_t wgs, unsigned threads)
+{
+    const uint64_t most = UINT32_MAX / threads;
+    return grid_for(wgs < most ? wgs : most);
+}
+
 hipError_t launch_fold_norm(const xred_fold_norm_args &a, hipStream_t stream);
 // Rows of the gradient's partial sums of dweight.
 uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden, uint64_t elem_size);

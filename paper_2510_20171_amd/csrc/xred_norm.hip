@@ -307,10 +307,11 @@ hipError_t go_norm(const NormParams &p, const void *const *srcs, unsigned thread
     NormSources<NP> src{};
     for (uint32_t i = 0; i < p.nsrc; ++i) src.p[i] = (const char *)srcs[i];
     const unsigned rows = rows_per_wg(L);
-    if (T::kVec == 4 && p.group == 512) threads = (threads + 127) / 128 * 128;
+    if (L) threads = 64 * kWaves;
+    else if (T::kVec == 4 && p.group == 512) threads = (threads + 127) / 128 * 128;
     return launch_kernel(fold_norm_kernel<T, NP, V, L>,
-                         dim3(grid_for((p.rows + rows - 1) / rows)),
-                         dim3(L ? 64 * kWaves : threads), 0, s, p, src);
+                         dim3(grid_of((p.rows + rows - 1) / rows, threads)), dim3(threads), 0, s,
+                         p, src);
 }
 
 // Threads for `pieces` pieces of a row, V each, in whole waves.

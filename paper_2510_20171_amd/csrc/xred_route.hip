@@ -447,7 +447,7 @@ hipError_t go_route(RouteParams p, bool sigmoid, hipStream_t s)
     p.group_lanes = p.per_group % V == 0 && (lanes & (lanes - 1)) == 0 && lanes < L ? lanes : 0;
     for (p.share = 1; 2 * p.share * p.groups <= L;) p.share *= 2;
     constexpr uint64_t per_wg = 64 / L * kWavesPerWg;
-    const dim3 grid(grid_for((p.tokens + per_wg - 1) / per_wg)), block(64 * kWavesPerWg);
+    const dim3 block(64 * kWavesPerWg), grid(grid_of((p.tokens + per_wg - 1) / per_wg, block.x));
     if (p.groups > 1)
         return sigmoid ? launch_kernel(route_kernel<T, L, V, true, true>, grid, block, 0, s, p)
                        : launch_kernel(route_kernel<T, L, V, false, true>, grid, block, 0, s, p);
@@ -615,7 +615,7 @@ template <class T, int L, int V>
 hipError_t go_route_grad(const RouteGradParams &p, bool sigmoid, hipStream_t s)
 {
     constexpr uint64_t per_wg = 64 / L * kWavesPerWg;
-    const dim3 grid(grid_for((p.tokens + per_wg - 1) / per_wg)), block(64 * kWavesPerWg);
+    const dim3 block(64 * kWavesPerWg), grid(grid_of((p.tokens + per_wg - 1) / per_wg, block.x));
     return sigmoid ? launch_kernel(route_grad_kernel<T, L, V, true>, grid, block, 0, s, p)
                    : launch_kernel(route_grad_kernel<T, L, V, false>, grid, block, 0, s, p);
 }
