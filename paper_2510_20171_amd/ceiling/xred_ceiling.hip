@@ -15,7 +15,8 @@
 // reduce kernel with the same mix is judged (P reads and one write for the
 // fused reduce, G reads and G writes for a simulated AllReduce in one
 // launch).  It also measures the host-to-kernel handoff of a flag in pinned
-// host memory (a ping-pong, below).
+// host memory (a ping-pong, below), and holds two kernels for tests: where a
+// launch's workgroups run, and the router's sigmoids over every input.
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -25,6 +26,7 @@
 #include <vector>
 
 #include "../csrc/xred_kernels.hpp"
+#include "../csrc/xred_sigmoid.hpp"
 
 namespace {
 
@@ -321,5 +323,65 @@ xred_ceiling_placement(uint32_t *out, unsigned grid, void *stream)
     if (out == nullptr || grid == 0) return (int)hipErrorInvalidValue;
     hipLaunchKernelGGL(placement_kernel, dim3(grid), dim3(kPlaceThreads), 0,
                        (hipStream_t)stream, out, grid);
+    return (int)hipGetLastError();
+}
+
+// ------------------------------------------------------------------ sigmoids --
+namespace {
+
+struct SigmoidCheck {
+    unsigned long long inputs, sigmoids, reciprocals;   // looked at; that differ
+    uint32_t first_sigmoid, first_reciprocal;           // the lowest bits that do
+};
+
+constexpr int kSigmoidValues = 16;   // a lane's, as in the widest router kernel
+
+// Every binary32 x: sigmoids() against sigmoid(); every 1 <= d < 2^126: reciprocal()
+// against the division.  NaN count as alike.
+__global__ __launch_bounds__(256) void sigmoid_kernel(SigmoidCheck *out)
+{
+    unsigned long long inputs = 0, s_bad = 0, r_bad = 0;
+    uint32_t s_first = ~0u, r_first = ~0u;
+    auto differ = [](float a, float b) {
+        return __float_as_uint(a) != __float_as_uint(b) && !(a != a && b != b);
+    };
+    for (uint64_t at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * kSigmoidValues; at >> 32 == 0;
+         at += (uint64_t)gridDim.x * 256 * kSigmoidValues) {
+        float x[kSigmoidValues], s[kSigmoidValues];
+#pragma unroll
+        for (uint32_t i = 0; i < kSigmoidValues; ++i) x[i] = __uint_as_float((uint32_t)at + i);
+        xred::sigmoids<kSigmoidValues>(x, s);
+#pragma unroll
+        for (uint32_t i = 0; i < kSigmoidValues; ++i) {
+            const uint32_t bits = (uint32_t)at + i;
+            ++inputs;
+            if (differ(s[i], xred::sigmoid(x[i]))) {
+                ++s_bad;
+                s_first = bits < s_first ? bits : s_first;
+            }
+            if (x[i] >= 1.0f && x[i] < 0x1p126f && differ(xred::reciprocal(x[i]), 1.0f / x[i])) {
+                ++r_bad;
+                r_first = bits < r_first ? bits : r_first;
+            }
+        }
+    }
+    atomicAdd(&out->inputs, inputs);
+    atomicAdd(&out->sigmoids, s_bad);
+    atomicAdd(&out->reciprocals, r_bad);
+    atomicMin(&out->first_sigmoid, s_first);
+    atomicMin(&out->first_reciprocal, r_first);
+}
+
+}  // namespace
+
+// Compares the router's sigmoids and reciprocals with their definitions, over every
+// input, and adds what it finds to *out (32 bytes of device memory, the counts zero and
+// the lowest bits ~0 before).  Stream-ordered; returns the hipError_t of the launch.
+extern "C" __attribute__((visibility("default"))) int
+xred_ceiling_sigmoids(void *out, void *stream)
+{
+    if (out == nullptr) return (int)hipErrorInvalidValue;
+    hipLaunchKernelGGL(sigmoid_kernel, dim3(4096), dim3(256), 0, (hipStream_t)stream,
+                       (SigmoidCheck *)out);
     return (int)hipGetLastError();
 }

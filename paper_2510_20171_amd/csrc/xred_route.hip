@@ -21,6 +21,7 @@
 // the registers, 57 us.)
 #include "xred_layer.hpp"
 #include "xred_rows.hpp"
+#include "xred_sigmoid.hpp"
 
 namespace xred {
 namespace {
@@ -52,8 +53,6 @@ __device__ __forceinline__ float value_of(int k)
 {
     return __int_as_float(k ^ ((k >> 31) & INT32_MAX));
 }
-
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
 
 // The first V experts from e on of a row: -inf past the last.  all: every lane's
 // V experts are there.
@@ -135,26 +134,6 @@ __device__ __forceinline__ void best_two_of(float &a, float &b)
     a = __uint_as_float(x.a);
     b = __uint_as_float(y.a);
     merge_two(a, b, __uint_as_float(x.b), __uint_as_float(y.b));
-}
-
-// 1 / (1 + exp(-x)) for V values, as sigmoid() rounds it.  The reciprocal's one
-// unit of error is taken out by a Newton step with fused multiply-adds, which
-// rounds correctly for every 1 <= d < 2^126; past that (x < -87.3) the quotient is
-// subnormal, and all V are divided.
-template <int V>
-__device__ __forceinline__ void sigmoids(const float (&x)[V], float (&s)[V])
-{
-    float most = 0.0f;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float d = 1.0f + expf(-x[i]), r = __builtin_amdgcn_rcpf(d);
-        s[i] = __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
-        most = __builtin_elementwise_maximum(most, d);
-        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // few registers, many waves
-    }
-    if (!(most < 0x1p126f))   // also for a NaN
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = sigmoid(x[i]);
 }
 
 constexpr int kGathered = 16;   // keys the lanes of a row can place
