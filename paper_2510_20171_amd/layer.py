@@ -68,6 +68,13 @@ def _slots(t, rows, topk, what, device, dtypes):
     return _vector(t, rows * topk, 4, what, device)
 
 
+def _count(n, what):
+    """n, which the C ABI takes as 32 bits."""
+    if not 0 <= n < 1 << 32:
+        _refuse(f"{what} = {n}")
+    return n
+
+
 def _score(name):
     if name not in SCORE:
         _refuse(f"unknown score {name!r}")
@@ -133,7 +140,7 @@ def fold_norm(srcs, out=None, *, residual=None, weight=None, sum=None, out8=None
         _refuse(f"out8 is {out8.dtype}, expected float8_e4m3fn or uint8")
     if scale is not None and _dtype_name(scale, None) != "f32":
         _refuse(f"scale is {scale.dtype}, expected float32")
-    groups = -(-hidden // group) if group > 0 else 1
+    groups = -(-hidden // group) if _count(group, "group") else 1
     w, wt = _weight(weight, dt, hidden, dev)
     ptrs = ptr_array([m.data or 0 for m in src])
     a = FoldNormArgs(
@@ -190,7 +197,8 @@ def route(logits, ids, weights, *, score: str = "softmax", bias=None, groups: in
     topk = _shape(ids, "ids")[1]
     dt, dev = _dtype_name(logits, None), logits.device
     a = RouteArgs(
-        tokens, experts, topk, groups, group_topk, group_score, ROUTE_RENORM if renorm else 0,
+        tokens, experts, topk, _count(groups, "groups"), _count(group_topk, "group_topk"),
+        _count(group_score, "group_score"), ROUTE_RENORM if renorm else 0,
         _matrix(logits, tokens, experts, ELEM_SIZE[dt], "logits", dev),
         _floats(bias, experts, "bias", dev), _slots(ids, tokens, topk, "ids", dev, ("i32",)),
         _slots(weights, tokens, topk, "weights", dev, ("f32",)), DTYPE[dt], _score(score), scale)
