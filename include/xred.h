@@ -505,6 +505,10 @@ enum { XRED_ROUTE_RENORM = 1u };   /* xred_route flags */
  *                 divided by their sum first (softmax: the softmax over the
  *                 chosen logits; scores that sum to 0 stay 0)
  * bias (a balance correction) steers the choice only, not the weights.
+ * With softmax it is added to the logits, and groups are ranked by logits too:
+ * a router that adds its bias to the probabilities p, or ranks groups by sums of
+ * them, chooses other experts.  That router is the sigmoid form on
+ * log(p / (1 - p)), whose score is p up to rounding (a p of 0 is then masked).
  *   logits   tokens x experts of dtype; bias: experts binary32, or NULL
  *   ids      tokens x topk int32;  weights: tokens x topk binary32
  *   experts  1..XRED_MAX_EXPERTS, topk 1..min(experts, XRED_MAX_TOPK), groups

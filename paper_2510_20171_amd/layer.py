@@ -188,7 +188,9 @@ def route(logits, ids, weights, *, score: str = "softmax", bias=None, groups: in
     best first, ids -1 and weight 0 where no expert is left.  score: "softmax" or
     "sigmoid"; bias (fp32, one an expert) steers the choice only; with groups > 1
     the group_topk best groups of experts are chosen from, ranked by their best
-    key (group_score = 1) or their best two."""
+    key (group_score = 1) or their best two.  The key is the sigmoid, or with softmax
+    the logit, plus the bias.  For a softmax router whose bias is added to its
+    probabilities p, route log(p / (1 - p)) with score="sigmoid"."""
     st = native().route(logits, ids, weights, score, bias, groups, group_topk, group_score,
                         renorm, scale, stream)
     if st is not None:   # plain tensors; anything else is checked below
