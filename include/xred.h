@@ -431,7 +431,9 @@ enum { XRED_MAX_EXPERTS = 1024, XRED_MAX_TOPK = 32, XRED_MAX_EXPERT_GROUPS = 64 
  *     sum    = down(h),  out = down(y)
  *     out8   = e4m3(y / scale),  scale = max(amax, 2^-100) / 448, amax the
  *              largest |y| of the group (a NaN in a group gives NaN)
- * h is not rounded before it is normalised.
+ * h is not rounded before it is normalised.  rstd, scale and y / scale are good to a
+ * few units in the last place of binary32 (hardware reciprocals and square root), so
+ * a y / scale that close to the middle of two e4m3 values may become either.
  *   srcs      host array of nsrc (1..XRED_MAX_SRC) device pointers, rows x
  *             hidden each, all with row distance src_stride; read before return
  *   residual  optional; weight: hidden elements of weight_dtype (dtype or

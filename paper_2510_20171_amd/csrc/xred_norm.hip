@@ -81,8 +81,10 @@ __device__ __forceinline__ void weight_piece(const char *w, bool wide, uint32_t 
 
 // Rows of 32 elements a thread leave no registers for the loads of one piece to
 // run ahead into the work on another, nor for what follows from a piece's place:
-// that is worked out anew at each use (2048 x 20000 bf16, one source: 117 -> 73 us,
-// the gradient 329 -> 179).
+// that is worked out anew at each use (2048 x 20000 bf16, one source, residual and sum:
+// 117 -> 73 us, 4.5 TB/s; the gradient with dsum 329 -> 179, 1.8 TB/s).  That leaves the
+// forward kernels without scratch; the gradient's of four and eight pieces, dweight's
+// sums among their values, still spill 9 to 20 of 128 registers.
 template <class T, int V>
 constexpr bool is_wide() { return V * T::kVec >= 32; }
 template <class T, int V>
@@ -150,8 +152,9 @@ __device__ __forceinline__ uint32_t row_of()
 }
 
 // 1 / 448 and 1 / scale are good to a unit in the last place, far inside e4m3's
-// half unit of 2^-4, and of a group's amax |y| / scale stays below 448 (1 + 2^-21),
-// which rounds to 448.
+// half unit of 2^-4: a quotient within some 2^-22 of the middle of two values may go to
+// the other one.  Of a group's amax |y| / scale stays below 448 (1 + 2^-21), which rounds
+// to 448.
 __device__ __forceinline__ float e4m3_scale(float amax)
 {
     return __builtin_elementwise_maximum(amax, 0x1p-100f) * (1.0f / 448.0f);
@@ -356,7 +359,8 @@ struct NormGradParams {
 // dweight sums over rows, dx over a row: the threads that hold a row keep their
 // columns' part of dweight in registers over all rows of a slice (the workgroup's
 // rows at slice, slice + slices, ...), so both come from one pass over dout and sum.
-// LEAN: rows too wide to wait in registers are read again, from the cache.
+// LEAN: rows too wide to wait in registers are read a second time, which makes wide rows
+// the farthest from their bytes (16384 x 4096 bf16 5.9 TB/s, 2048 x 20000 1.8).
 template <class T, int V, int L, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradParams p)
 {
@@ -560,11 +564,12 @@ hipError_t go_grad_shape(const NormGradParams &p, hipStream_t s)
 // As many slices as put some 12 waves on each CU, where HBM delivers the most beside
 // three streams that are read (16384 x 4096 bf16, 8 / 12 / 16 / 24 waves: 111 / 90 / 93 /
 // 102 us), in whole workgroups where few make them up (8192 x 5120 bf16, 512 / 614 / 768
-// workgroups of 5 waves: 61 / 86 / 74 us), but at least 4 rows a slice, which keeps the
-// partial sums' traffic below the rows' (2048 x 768, 2 / 4 / 8 rows: 11.7 / 12.2 / 15.8 us;
-// 1024 x 8192: 23.1 / 21.4 / 21.5).  Short rows: the waves of a workgroup
-// join their sums in LDS, a quarter of the parts or fewer (65536 x 512 bf16: 48 us, a
-// part a wave 63).
+// workgroups of 5 waves: 61 / 86 / 74 us).  From 1024 rows on a slice has at least 4, which
+// keeps the partial sums' traffic below the rows' (2048 x 768, 2 / 4 / 8 rows: 11.7 / 12.2 /
+// 15.8 us; 1024 x 8192: 23.1 / 21.4 / 21.5); fewer rows make 256 slices, or one each below
+// 256, where the launch and one workgroup's chain count and not the traffic.  Short rows:
+// the waves of a workgroup join their sums in LDS, a quarter of the parts or fewer (65536 x
+// 512 bf16: 48 us, a part a wave 63).
 uint32_t norm_grad_slices(uint64_t rows, uint64_t hidden, uint64_t es)
 {
     const int lanes = grad_lanes(hidden);
