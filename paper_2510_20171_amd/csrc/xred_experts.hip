@@ -4,10 +4,10 @@
 //
 // Copies, reduction and gradient are bound by HBM: dispatch of 16384 x 4096 e4m3
 // with scales, top 8, a tenth dropped 107 us, 5.3 TB/s (1 stream in, 8 out: 5.3);
-// combine of 12288 x 4096 bf16, top 8, onto a base 165 us, 6.1 TB/s (9 in, 1 out:
-// 6.8); its gradient for 4096 x 2501 fp32, top 4, a tenth dropped 68 us, 4.9 TB/s
+// combine of 12288 x 4096 bf16, top 8, onto a base 167 us, 6.0 TB/s (9 in, 1 out:
+// 6.8); its gradient for 4096 x 2501 fp32, top 4, a tenth dropped 68 us, 5.0 TB/s
 // (rows of 2496, which start on the 16-byte grid: 63 us, 5.3).  The plan is bound by
-// its chain of launches, barriers and loads: 488 slots 4 us, 131072 slots 11 us.
+// its chain of launches, barriers and loads: 488 slots 4 us, 131072 slots 10-12 us.
 #include "xred_layer.hpp"
 #include "xred_rows.hpp"
 

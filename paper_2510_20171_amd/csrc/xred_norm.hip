@@ -8,11 +8,11 @@
 // rstd * max |h * weight|, so it comes out of the same reduction.
 //
 // Bound by HBM from some hundred rows on: 8192 x 4096 bf16, 8 sources, residual, sum,
-// bf16 and 8-bit outputs 129 us, 6.0 TB/s (a kernel that only moves 9 such streams in
+// bf16 and 8-bit outputs 131 us, 5.9 TB/s (a kernel that only moves 9 such streams in
 // and 2.5 out: 6.4); one source with an 8-bit output 47 us, 5.0 TB/s; 131072 x 128
 // bf16, one source, residual and sum 25 us (a wave a row: 71); 1999 x 5003 fp16, two
-// sources 22 us, 4.5 TB/s, from the 256 MB cache.  The gradient of 16384 x 4096 bf16 90
-// us, 5.9 TB/s (3 streams in, 1 out: 6.4).  One row takes 4.3 us, most of it the
+// sources 23 us, 4.4 TB/s, from the 256 MB cache.  The gradient of 16384 x 4096 bf16 92
+// us, 5.8 TB/s (3 streams in, 1 out: 6.4).  One row takes 4.8 us, 3.1 of it the
 // launch.  (Keeping the next row's loads in flight while one is worked on made the
 // gradient slower, 96 us at best: a wait for loads also waits for the stores before
 // them.)
@@ -360,7 +360,7 @@ struct NormGradParams {
 // columns' part of dweight in registers over all rows of a slice (the workgroup's
 // rows at slice, slice + slices, ...), so both come from one pass over dout and sum.
 // LEAN: rows too wide to wait in registers are read a second time, which makes wide rows
-// the farthest from their bytes (16384 x 4096 bf16 5.9 TB/s, 2048 x 20000 1.8).
+// the farthest from their bytes (16384 x 4096 bf16 5.8 TB/s, 2048 x 20000 1.8).
 template <class T, int V, int L, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradParams p)
 {
