@@ -103,3 +103,31 @@ def test_calls_leave_temporaries_of_the_current_stream_alone(xr, which):
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
         torch.cuda.synchronize()
         assert bool((seen == 0x5A).all())
+
+
+@pytest.mark.gpu
+def test_a_captured_call_on_a_named_stream(xr):
+    """Its workspace comes from the graph's memory: replays give the same, whatever is
+    allocated and written between them."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    tokens, k, experts = 5000, 8, 300
+    ids = torch.randint(-1, experts, (tokens, k), device="cuda", generator=g).int()
+    outs = [torch.empty(n, dtype=torch.int32, device="cuda") for n in (experts, experts + 1)]
+    outs.append(torch.empty_like(ids))
+    xr.dispatch_plan(ids, *outs)
+    want = [t.clone() for t in outs]
+    need = xr.load().xred_dispatch_plan_workspace(tokens * k, experts)
+    torch.cuda.synchronize()
+    for handle in (False, True):
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            xr.dispatch_plan(ids, *outs, stream=side.cuda_stream if handle else side)
+        for n in range(3):
+            for t in outs:
+                t.fill_(n)
+            other = [torch.full((need,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(4)]
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, want)), (handle, n)
+            assert all(bool((t == 0x5A).all()) for t in other)
