@@ -32,6 +32,7 @@ __all__ = ["allreduce_local", "reduce_scatter_local", "reduce_copy_step", "acc_c
            "set_max_workgroups", "stream_create_partition", "stream_destroy", "pack_items", "acc_elem_size", "version", "release",
            "fold_norm", "fold_norm_grad", "route", "route_grad",
            "dispatch_plan", "dispatch", "combine", "combine_grad",
+           "group_product", "group_product_grad", "gate", "gate_grad", "quant_mx4", "dequant_mx4",
            "XredError", "load", "EXPORTS"]
 
 
@@ -303,3 +304,5 @@ def release() -> None:
 
 from .layer import (combine, combine_grad, dispatch, dispatch_plan, fold_norm,  # noqa: E402
                     fold_norm_grad, route, route_grad)   # they use the helpers above
+from .products import (dequant_mx4, gate, gate_grad, group_product,  # noqa: E402
+                       group_product_grad, quant_mx4)

@@ -75,6 +75,17 @@ CombineArgs = _struct("CombineArgs", [
     "q tokens hidden y_rows", "u topk", "i dtype", "r y base out", "p pos weights"])
 CombineGradArgs = _struct("CombineGradArgs", [
     "q tokens hidden y_rows", "u topk", "i dtype", "r dout y dy", "p pos weights dweights"])
+GroupProductArgs = _struct("GroupProductArgs", [
+    "q rows n k", "u experts flags", "i dtype out_dtype", "r x scale w w_scale out",
+    "q w_expert w_scale_expert", "p offsets"])
+GroupProductGradArgs = _struct("GroupProductGradArgs", [
+    "q rows n k", "u experts flags", "i dtype dw_dtype", "r dout x dw", "q dw_expert", "p offsets"])
+GateArgs = _struct("GateArgs", [
+    "q rows width", "u group", "i dtype", "r x out out8 scale", "p count"])
+GateGradArgs = _struct("GateGradArgs", ["q rows width", "i dtype", "r dout x dx", "p count"])
+QuantMx4Args = _struct("QuantMx4Args", ["q rows columns", "i dtype", "r x out4 scale"])
+DequantMx4Args = _struct("DequantMx4Args", ["q rows columns", "i dtype", "r x4 scale out"])
+PRODUCT_TRANSPOSE, PRODUCT_MX4, PRODUCT_ADD = 1, 2, 1
 SCORE = {"softmax": 0, "sigmoid": 1}
 ROUTE_RENORM = 1
 
@@ -86,6 +97,8 @@ EXPORTS = ("xred_allreduce_local", "xred_reduce_scatter_local", "xred_reduce_cop
            "xred_route", "xred_route_grad",
            "xred_dispatch_plan", "xred_dispatch_plan_workspace", "xred_dispatch",
            "xred_combine", "xred_combine_grad",
+           "xred_group_product", "xred_group_product_grad", "xred_gate", "xred_gate_grad",
+           "xred_quant_mx4", "xred_dequant_mx4",
            "xred_set_max_workgroups",
            "xred_stream_create_partition", "xred_stream_destroy", "xred_acc_elem_size",
            "xred_status_string",
@@ -141,7 +154,9 @@ def load(path: Path = LIB_PATH) -> ctypes.CDLL:
     L.xred_stream_create_partition.argtypes = [i32, ctypes.POINTER(vp), ctypes.POINTER(vp)]
     L.xred_stream_destroy.argtypes = [vp]
     for f in ("xred_fold_norm", "xred_fold_norm_grad", "xred_route", "xred_route_grad",
-              "xred_dispatch_plan", "xred_dispatch", "xred_combine", "xred_combine_grad"):
+              "xred_dispatch_plan", "xred_dispatch", "xred_combine", "xred_combine_grad",
+              "xred_group_product", "xred_group_product_grad", "xred_gate", "xred_gate_grad",
+              "xred_quant_mx4", "xred_dequant_mx4"):
         getattr(L, f).argtypes = [vp, vp]
         getattr(L, f).restype = ctypes.c_int
     L.xred_fold_norm_grad_workspace.argtypes = [ctypes.c_uint64, ctypes.c_uint64]

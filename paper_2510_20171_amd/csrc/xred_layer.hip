@@ -1,7 +1,13 @@
 // xred_layer.hip -- the C ABI of the calls around a reduced activation:
 // argument checks and dispatch to the launchers (xred_norm.hip, xred_route.hip,
-// xred_experts.hip).  As elsewhere, everything is checked before anything is enqueued.
+// xred_experts.hip, xred_product_*.hip, xred_gate.hip, xred_mx4.hip).  As elsewhere, everything is checked before anything is enqueued.
 #include "xred_layer.hpp"
+
+#define TRY(call)                                    \
+    do {                                             \
+        const xred_status st_ = (call);              \
+        if (st_ != XRED_SUCCESS) return st_;         \
+    } while (0)
 
 namespace xred {
 namespace {
@@ -102,6 +108,50 @@ xred_status check_slots(uint64_t tokens, uint32_t topk, uint64_t hidden, uint64_
     return XRED_SUCCESS;
 }
 
+// What the experts' products share: sizes.  `tiles`: the most that a launch has, of the
+// smallest kind.
+xred_status check_product(uint64_t rows, uint64_t n, uint64_t k, uint32_t experts, bool grad)
+{
+    if (experts < 1 || experts > XRED_MAX_EXPERTS)
+        return fail(XRED_UNSUPPORTED, "experts = %u outside 1..%d", experts, XRED_MAX_EXPERTS);
+    if (n < 1 || n > XRED_MAX_PRODUCT || k < 1 || k > XRED_MAX_PRODUCT)
+        return fail(XRED_UNSUPPORTED, "n = %llu, k = %llu outside 1..%d", (unsigned long long)n,
+                    (unsigned long long)k, XRED_MAX_PRODUCT);
+    if (rows > INT32_MAX)
+        return fail(XRED_UNSUPPORTED, "rows = %llu, at most 2^31 - 1 are supported",
+                    (unsigned long long)rows);
+    const uint64_t tiles = grad ? experts * ((n + 63) / 64) * ((k + 63) / 64)
+                                : (rows / 16 + experts) * ((n + 31) / 32);
+    if (tiles > INT32_MAX / 2)
+        return fail(XRED_UNSUPPORTED, "an output of %llu tiles", (unsigned long long)tiles);
+    return XRED_SUCCESS;
+}
+
+// What the calls on every element of a row share.
+xred_status check_elements(uint64_t rows, uint64_t columns, const char *name)
+{
+    if (columns < 1 || columns > XRED_MAX_PRODUCT)
+        return fail(XRED_UNSUPPORTED, "%s = %llu outside 1..%d", name, (unsigned long long)columns,
+                    XRED_MAX_PRODUCT);
+    if (rows > INT32_MAX || rows * ((columns + 511) / 512) > INT32_MAX)
+        return fail(XRED_UNSUPPORTED, "rows = %llu of %llu elements", (unsigned long long)rows,
+                    (unsigned long long)columns);
+    return XRED_SUCCESS;
+}
+
+// Matrices of `each` rows, one for every expert, `apart` elements from one another.
+xred_status check_stack(const xred_rows &m, uint64_t apart, uint32_t experts, uint64_t each,
+                        uint64_t columns, uint64_t es, const char *name, Matrix *out)
+{
+    TRY(check_rows(m, each, columns, es, name, out));
+    uint64_t far, bytes;
+    if (__builtin_mul_overflow(apart, es, &bytes) || __builtin_mul_overflow(bytes, (uint64_t)(experts - 1), &far) ||
+        __builtin_add_overflow(far, out->span(), &far) || far > (uint64_t)INT64_MAX)
+        return fail(XRED_INVALID_ARGUMENT, "%s: size overflows", name);
+    *out = Matrix{m.data, far, far, 1};
+    return check_buf(m.data, far, es, name, 0);
+}
+
 xred_status check_words(const void *p, uint64_t tokens, uint64_t topk, const char *name, Matrix *out)
 {
     return check_rows(xred_rows{(void *)p, topk}, tokens, topk, 4, name, out);
@@ -111,12 +161,6 @@ xred_status check_words(const void *p, uint64_t tokens, uint64_t topk, const cha
 }  // namespace xred
 
 using namespace xred;
-
-#define TRY(call)                                    \
-    do {                                             \
-        const xred_status st_ = (call);              \
-        if (st_ != XRED_SUCCESS) return st_;         \
-    } while (0)
 
 extern "C" {
 
@@ -419,6 +463,197 @@ XRED_API xred_status xred_combine_grad(const xred_combine_grad_args *args, void 
     TRY(check_apart(out, names, nout, in, nin, may));
     const hipError_t e = launch_combine_grad(a, (hipStream_t)hip_stream);
     return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "combine_grad launch");
+}
+
+XRED_API xred_status xred_group_product(const xred_group_product_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_group_product_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_group_product rows=%llu n=%llu k=%llu experts=%u dtype=%d out_dtype=%d "
+                     "flags=0x%x stream=%p", (unsigned long long)a.rows, (unsigned long long)a.n,
+                     (unsigned long long)a.k, a.experts, (int)a.dtype, (int)a.out_dtype, a.flags,
+                     hip_stream);
+    if (a.flags & ~(unsigned)(XRED_PRODUCT_TRANSPOSE | XRED_PRODUCT_MX4))
+        return fail(XRED_INVALID_ARGUMENT, "unknown flag bits 0x%x", a.flags);
+    const bool mx4 = a.flags & XRED_PRODUCT_MX4, e4m3 = a.dtype == XRED_FP8_E4M3 && !mx4;
+    const bool across = a.flags & XRED_PRODUCT_TRANSPOSE;
+    if (mx4 ? a.dtype != XRED_UINT8 : !row_type(a.dtype) && !e4m3)
+        return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    if (!row_type(a.out_dtype) ||
+        (!mx4 && !e4m3 && a.out_dtype != a.dtype && a.out_dtype != XRED_FLOAT32))
+        return fail(XRED_UNSUPPORTED, "out_dtype %d with dtype %d", (int)a.out_dtype, (int)a.dtype);
+    if (across && (mx4 || e4m3))
+        return fail(XRED_UNSUPPORTED, "scaled weights cannot be transposed");
+    TRY(check_product(a.rows, a.n, a.k, a.experts, false));
+    if (a.rows == 0) return XRED_SUCCESS;
+    Matrix in[5], out[1];
+    const char *const names[1] = {"out"};
+    const int may[1] = {0};
+    int nin = 0;
+    const uint64_t es = elem_size(a.dtype), k = mx4 ? (a.k + 31) / 32 * 16 : a.k;
+    TRY(check_rows(a.x, a.rows, k, es, "x", &in[nin++]));
+    TRY(check_stack(a.w, a.w_expert, a.experts, across ? a.k : a.n, across ? a.n : k, es, "w",
+                    &in[nin++]));
+    if (mx4 || e4m3) {
+        const uint64_t by = mx4 ? 32 : XRED_SCALE_BLOCK, parts = (a.k + by - 1) / by;
+        const uint64_t ss = mx4 ? 1 : 4, w_rows = mx4 ? a.n : (a.n + by - 1) / by;
+        TRY(check_rows(a.scale, a.rows, parts, ss, "scale", &in[nin++]));
+        TRY(check_stack(a.w_scale, a.w_scale_expert, a.experts, w_rows, parts, ss, "w_scale",
+                        &in[nin++]));
+    } else if (a.scale.data || a.w_scale.data) {
+        return fail(XRED_INVALID_ARGUMENT, "dtype %d has no scales", (int)a.dtype);
+    }
+    TRY(check_words(a.offsets, 1, a.experts + 1, "offsets", &in[nin++]));
+    TRY(check_rows(a.out, a.rows, a.n, elem_size(a.out_dtype), "out", &out[0]));
+    TRY(check_apart(out, names, 1, in, nin, may));
+    const hipError_t e = launch_group_product(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "group_product launch");
+}
+
+XRED_API xred_status xred_group_product_grad(const xred_group_product_grad_args *args,
+                                             void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_group_product_grad_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_group_product_grad rows=%llu n=%llu k=%llu experts=%u dtype=%d "
+                     "dw_dtype=%d flags=0x%x stream=%p", (unsigned long long)a.rows,
+                     (unsigned long long)a.n, (unsigned long long)a.k, a.experts, (int)a.dtype,
+                     (int)a.dw_dtype, a.flags, hip_stream);
+    if (a.flags & ~(unsigned)XRED_PRODUCT_ADD)
+        return fail(XRED_INVALID_ARGUMENT, "unknown flag bits 0x%x", a.flags);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    if (a.dw_dtype != a.dtype && a.dw_dtype != XRED_FLOAT32)
+        return fail(XRED_UNSUPPORTED, "dw_dtype %d with dtype %d", (int)a.dw_dtype, (int)a.dtype);
+    TRY(check_product(a.rows, a.n, a.k, a.experts, true));
+    Matrix in[3], out[1];
+    const char *const names[1] = {"dw"};
+    const int may[1] = {0};
+    int nin = 0;
+    const uint64_t es = elem_size(a.dtype), dw_es = elem_size(a.dw_dtype);
+    if (a.rows) {
+        TRY(check_rows(a.dout, a.rows, a.n, es, "dout", &in[nin++]));
+        TRY(check_rows(a.x, a.rows, a.k, es, "x", &in[nin++]));
+    }
+    TRY(check_words(a.offsets, 1, a.experts + 1, "offsets", &in[nin++]));
+    Matrix one;
+    TRY(check_rows(a.dw, a.n, a.k, dw_es, "dw", &one));
+    if (a.experts > 1 && a.dw_expert < (a.n - 1) * a.dw.stride + a.k)
+        return fail(XRED_INVALID_ARGUMENT, "dw: experts %llu elements apart overlap",
+                    (unsigned long long)a.dw_expert);
+    TRY(check_stack(a.dw, a.dw_expert, a.experts, a.n, a.k, dw_es, "dw", &out[0]));
+    TRY(check_apart(out, names, 1, in, nin, may));
+    if (a.rows == 0 && (a.flags & XRED_PRODUCT_ADD)) return XRED_SUCCESS;
+    const hipError_t e = launch_group_product_grad(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "group_product_grad launch");
+}
+
+XRED_API xred_status xred_gate(const xred_gate_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_gate_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_gate rows=%llu width=%llu dtype=%d group=%u stream=%p",
+                     (unsigned long long)a.rows, (unsigned long long)a.width, (int)a.dtype, a.group,
+                     hip_stream);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    TRY(check_elements(a.rows, a.width, "width"));
+    if (a.out8.data && (a.group < 32 || a.group > 512 || (a.group & (a.group - 1))))
+        return fail(XRED_INVALID_ARGUMENT, "group = %u is not 32, 64, 128, 256 or 512", a.group);
+    if (a.rows == 0) return XRED_SUCCESS;
+    if (!a.out.data && !a.out8.data)
+        return fail(XRED_INVALID_ARGUMENT, "neither out nor out8 is given");
+    if ((a.out8.data == nullptr) != (a.scale.data == nullptr))
+        return fail(XRED_INVALID_ARGUMENT, "out8 and scale go together");
+    Matrix in[2], out[3];
+    const char *names[3];
+    int nin = 0, nout = 0;
+    const int may[3] = {0, 0, 0};
+    const uint64_t es = elem_size(a.dtype);
+    TRY(check_rows(a.x, a.rows, 2 * a.width, es, "x", &in[nin++]));
+    if (a.count) TRY(check_words(a.count, 1, 1, "count", &in[nin++]));
+    auto output = [&](const xred_rows &m, uint64_t columns, uint64_t size, const char *name) {
+        names[nout] = name;
+        return m.data ? check_rows(m, a.rows, columns, size, name, &out[nout++]) : XRED_SUCCESS;
+    };
+    TRY(output(a.out, a.width, es, "out"));
+    TRY(output(a.out8, a.width, 1, "out8"));
+    if (a.out8.data) TRY(output(a.scale, (a.width + a.group - 1) / a.group, 4, "scale"));
+    TRY(check_apart(out, names, nout, in, nin, may));
+    const hipError_t e = launch_gate(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "gate launch");
+}
+
+XRED_API xred_status xred_gate_grad(const xred_gate_grad_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_gate_grad_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_gate_grad rows=%llu width=%llu dtype=%d stream=%p",
+                     (unsigned long long)a.rows, (unsigned long long)a.width, (int)a.dtype,
+                     hip_stream);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    TRY(check_elements(a.rows, a.width, "width"));
+    if (a.rows == 0) return XRED_SUCCESS;
+    Matrix in[3], out[1];
+    const char *const names[1] = {"dx"};
+    const int may[1] = {1};
+    int nin = 0;
+    const uint64_t es = elem_size(a.dtype);
+    TRY(check_rows(a.x, a.rows, 2 * a.width, es, "x", &in[nin++]));
+    TRY(check_rows(a.dout, a.rows, a.width, es, "dout", &in[nin++]));
+    if (a.count) TRY(check_words(a.count, 1, 1, "count", &in[nin++]));
+    TRY(check_rows(a.dx, a.rows, 2 * a.width, es, "dx", &out[0]));
+    TRY(check_apart(out, names, 1, in, nin, may));
+    const hipError_t e = launch_gate_grad(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "gate_grad launch");
+}
+
+XRED_API xred_status xred_quant_mx4(const xred_quant_mx4_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_quant_mx4_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_quant_mx4 rows=%llu columns=%llu dtype=%d stream=%p",
+                     (unsigned long long)a.rows, (unsigned long long)a.columns, (int)a.dtype,
+                     hip_stream);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    TRY(check_elements(a.rows, a.columns, "columns"));
+    if (a.rows == 0) return XRED_SUCCESS;
+    Matrix in[1], out[2];
+    const char *const names[2] = {"out4", "scale"};
+    const int may[2] = {0, 0};
+    const uint64_t blocks = (a.columns + 31) / 32;
+    TRY(check_rows(a.x, a.rows, a.columns, elem_size(a.dtype), "x", &in[0]));
+    TRY(check_rows(a.out4, a.rows, blocks * 16, 1, "out4", &out[0]));
+    TRY(check_rows(a.scale, a.rows, blocks, 1, "scale", &out[1]));
+    TRY(check_apart(out, names, 2, in, 1, may));
+    const hipError_t e = launch_quant_mx4(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "quant_mx4 launch");
+}
+
+XRED_API xred_status xred_dequant_mx4(const xred_dequant_mx4_args *args, void *hip_stream)
+{
+    if (args == nullptr) return fail(XRED_INVALID_ARGUMENT, "args is NULL");
+    const xred_dequant_mx4_args &a = *args;
+    if (trace_enabled())
+        trace_printf("xred_dequant_mx4 rows=%llu columns=%llu dtype=%d stream=%p",
+                     (unsigned long long)a.rows, (unsigned long long)a.columns, (int)a.dtype,
+                     hip_stream);
+    if (!row_type(a.dtype)) return fail(XRED_UNSUPPORTED, "dtype %d", (int)a.dtype);
+    TRY(check_elements(a.rows, a.columns, "columns"));
+    if (a.rows == 0) return XRED_SUCCESS;
+    Matrix in[2], out[1];
+    const char *const names[1] = {"out"};
+    const int may[1] = {0};
+    const uint64_t blocks = (a.columns + 31) / 32;
+    TRY(check_rows(a.x4, a.rows, blocks * 16, 1, "x4", &in[0]));
+    TRY(check_rows(a.scale, a.rows, blocks, 1, "scale", &in[1]));
+    TRY(check_rows(a.out, a.rows, a.columns, elem_size(a.dtype), "out", &out[0]));
+    TRY(check_apart(out, names, 1, in, 2, may));
+    const hipError_t e = launch_dequant_mx4(a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? XRED_SUCCESS : hip_fail(e, "dequant_mx4 launch");
 }
 
 }  // extern "C"

@@ -1,5 +1,6 @@
 // xred_layer.hpp -- launchers behind the calls around a reduced activation
-// (norm, routing, dispatch, combine).  Arguments were validated by the caller
+// (norm, routing, dispatch, combine, and the
+// experts' products and activation between the last two).  Arguments were validated by the caller
 // (xred_layer.hip).
 #pragma once
 
@@ -30,5 +31,12 @@ hipError_t launch_dispatch_plan(const xred_dispatch_plan_args &a, hipStream_t st
 hipError_t launch_dispatch(const xred_dispatch_args &a, hipStream_t stream);
 hipError_t launch_combine(const xred_combine_args &a, hipStream_t stream);
 hipError_t launch_combine_grad(const xred_combine_grad_args &a, hipStream_t stream);
+
+hipError_t launch_group_product(const xred_group_product_args &a, hipStream_t stream);
+hipError_t launch_group_product_grad(const xred_group_product_grad_args &a, hipStream_t stream);
+hipError_t launch_gate(const xred_gate_args &a, hipStream_t stream);
+hipError_t launch_gate_grad(const xred_gate_grad_args &a, hipStream_t stream);
+hipError_t launch_quant_mx4(const xred_quant_mx4_args &a, hipStream_t stream);
+hipError_t launch_dequant_mx4(const xred_dequant_mx4_args &a, hipStream_t stream);
 
 }  // namespace xred

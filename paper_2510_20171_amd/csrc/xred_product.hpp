@@ -1,0 +1,585 @@
+// xred_product.hpp -- the experts' matrix products over ragged rows on the matrix
+// cores: device code of xred_group_product and xred_group_product_grad.
+//
+// Both are tiles of D[row][column] = sum over k of R[row][k] * C[column][k], where R
+// and C are two operands whose rows lie along k, or across it (k counts their rows):
+//     forward     R = x (along),      C = w (along; across when transposed)
+//     gradient    R = dout (across),  C = x (across), k an expert's rows
+// Operand bytes go through LDS in steps of 128 bytes of k for each row (64 elements
+// of 2 bytes, 32 of fp32, 128 of e4m3, 256 of mx4), so that every type runs the same
+// code around its matrix instruction.
+//
+// Layout of a step in LDS: along, each row's eight 16-byte pieces in order of
+// piece ^ (row % 8), so that eight neighbouring rows' pieces of one place lie in
+// different banks; across, rows of k as they lie in memory, 16-bit ones in pairs of
+// pieces in order of pair ^ (row % 4), for the transposing reads.
+//
+// A fragment is 16 bytes of a lane: lane l holds row l % 32 of a block of 32 and, in
+// sub-step s of four, piece 4 * (l / 32) + s of the step.  Any order of k serves, as
+// long as both operands keep to it; this one gives a lane the dword of an mx4 row's
+// eight exponents that its pieces need.
+#pragma once
+
+#include "xred_product_launch.hpp"
+#include "xred_rows.hpp"
+
+namespace xred {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char *lds_bytes;
+
+// Operand types: bytes of an element (mx4: of two), elements of k in a step.
+struct PBF16 {
+    static constexpr int kSize = 2, kStep = 64;
+};
+struct PF16 {
+    static constexpr int kSize = 2, kStep = 64;
+};
+struct PF32 {
+    static constexpr int kSize = 4, kStep = 32;
+};
+struct PE4M3 {
+    static constexpr int kSize = 1, kStep = 128;
+};
+struct PMx4 {
+    static constexpr int kSize = 1, kStep = 128;   // counted in bytes
+};
+
+constexpr int kProductThreads = 256;
+
+// acc += columns' fragment (32 columns) * rows' fragment (32 rows): lane l has row
+// l % 32 and, in registers 4 q .. 4 q + 3, columns 8 q + 4 (l / 32) and the next three.
+template <class P>
+__device__ __forceinline__ f32x16 multiply(u32x4 c, u32x4 r, f32x16 acc)
+{
+    if constexpr (__is_same(P, PBF16)) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, c),
+                                                       __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
+    } else if constexpr (__is_same(P, PF16)) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, c),
+                                                      __builtin_bit_cast(f16x8, r), acc, 0, 0, 0);
+    } else {
+        static_assert(__is_same(P, PF32));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(c[j]), __uint_as_float(r[j]),
+                                                       acc, 0, 0, 0);
+        return acc;
+    }
+}
+
+__device__ __forceinline__ i32x8 two(u32x4 a, u32x4 b)
+{
+    return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+// Two fragments of e4m3, 64 elements of k, times 1 (the exponent 127 in every byte).
+__device__ __forceinline__ f32x16 multiply_e4m3(u32x4 c0, u32x4 c1, u32x4 r0, u32x4 r1, f32x16 acc)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(two(c0, c1), two(r0, r1), acc, 0, 0, 0,
+                                                           0x7F7F7F7F, 0, 0x7F7F7F7F);
+}
+
+// A fragment of e2m1, 64 elements of k; byte S of cs and rs holds the exponents.
+template <int S>
+__device__ __forceinline__ f32x16 multiply_mx4(u32x4 c, u32x4 r, uint32_t cs, uint32_t rs, f32x16 acc)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(two(c, u32x4{}), two(r, u32x4{}), acc, 4,
+                                                           4, S, (int)cs, S, (int)rs);
+}
+
+// What loads past the end of k read instead.
+__device__ const u32x4 product_zeros = {0, 0, 0, 0};
+
+// ---------------------------------------------------------------- operands --
+// One operand's pieces of a tile of N rows (along) or columns (across): kPieces a
+// thread and step, on their way into LDS or into registers.
+template <class P, bool ACROSS, bool DIRECT, int N>
+struct Operand {
+    static constexpr int kPieces = N * 128 / 16 / kProductThreads;
+    static constexpr int kWide = N * P::kSize / 16;   // across: pieces of a row of k
+    static constexpr int kRows = 128 / P::kSize;      // across: rows of k in a step
+    static constexpr int kPer = 16 / P::kSize;        // elements of a piece
+
+    const char *base;
+    uint64_t step;            // bytes from one step to the next
+    uint64_t at[kPieces];     // from base: this thread's pieces
+    uint32_t k[kPieces];      // along: byte of k within a step; across: row of k
+    int32_t have[kPieces];    // across: bytes of the piece that exist, below 0 none
+    u32x4 held[DIRECT ? 1 : kPieces];
+
+    static __device__ __forceinline__ uint32_t slot(int i)
+    {
+        return ((threadIdx.x / 64) * kPieces + i) * 64 + threadIdx.x % 64;
+    }
+
+    // items: rows (along) or columns (across) that exist, at least one; those
+    // behind them are read as others, whose products nobody stores.
+    __device__ __forceinline__ void start(const char *from, uint64_t stride, uint32_t items)
+    {
+        base = from;
+        step = ACROSS ? stride * kRows : 128;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t q = slot(i);
+            if constexpr (ACROSS) {
+                const uint32_t row = q / kWide;
+                uint32_t piece = q % kWide;
+                if constexpr (P::kSize == 2) piece ^= (row % 4) * 2;
+                const int32_t left = (int32_t)(items * P::kSize) - (int32_t)piece * 16;
+                k[i] = row;
+                have[i] = left;
+                at[i] = row * stride + (left > 0 ? piece * 16 : 0);
+            } else {
+                const uint32_t row = q / 8, piece = q % 8 ^ row % 8;
+                k[i] = piece * 16;
+                at[i] = (row < items ? row : items - 1) * stride + piece * 16;
+            }
+        }
+    }
+
+    // Step t of k into `to` (DIRECT) or into registers.  length: of k, in bytes
+    // (along) or rows (across).
+    __device__ __forceinline__ void load(uint32_t t, uint32_t length, lds_bytes to)
+    {
+        const uint32_t done = t * (ACROSS ? kRows : 128), left = length - done;
+        const bool whole = left >= (ACROSS ? kRows : 128);
+        const char *from = base + t * step;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            if constexpr (DIRECT) {
+                const char *src = from + at[i];
+                if (!whole && k[i] >= left) src = (const char *)&product_zeros;
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void *)src,
+                    (__attribute__((address_space(3))) void *)(to + ((threadIdx.x / 64) * kPieces + i) * 1024),
+                    16, 0, 0);
+            } else {
+                const char *src = from + at[i];
+                int32_t bytes = ACROSS ? (k[i] < left ? have[i] : 0) : (int32_t)left - (int32_t)k[i];
+                if (bytes >= 16) {
+                    held[i] = *(const __attribute__((address_space(1))) u32x4_any *)(global_bytes)src;
+                } else {
+                    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)
+                        if (j * P::kSize < bytes) {
+                            if constexpr (P::kSize == 4)
+                                v[j] = *(const uint32_t *)(src + j * 4);
+                            else if constexpr (P::kSize == 2)
+                                v[j / 2] |= (uint32_t)*(const uint16_t *)(src + j * 2) << (16 * (j % 2));
+                            else
+                                v[j / 4] |= (uint32_t)*(const uint8_t *)(src + j) << (8 * (j % 4));
+                        }
+                    held[i] = v;
+                }
+            }
+        }
+    }
+
+    // What load() left in registers, to LDS.
+    __device__ __forceinline__ void store(lds_bytes to) const
+    {
+        if constexpr (!DIRECT)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                *(__attribute__((address_space(3))) u32x4 *)(to + slot(i) * 16) = held[i];
+    }
+
+    // Sub-step s of block b of 32.
+    static __device__ __forceinline__ u32x4 fragment(lds_bytes from, int b, int s)
+    {
+        const uint32_t l = threadIdx.x % 64, h = l / 32;
+        if constexpr (!ACROSS) {
+            return *(const __attribute__((address_space(3))) u32x4 *)(
+                from + b * 4096 + l % 32 * 128 + ((4 * h + s) ^ l % 8) * 16);
+        } else if constexpr (P::kSize == 2) {
+            // 16 lanes read 4 rows of 16 columns: lane i gets column i of them
+            const uint32_t i = l % 16, row = 8 * (4 * h + s) + i / 4;
+            const uint32_t piece = (b * 4 + l / 16 % 2 * 2 + i % 4 / 2) ^ (i / 4 * 2);
+            const lds_bytes p = from + row * (N * 2) + piece * 16 + i % 2 * 8;
+            using Read = __attribute__((address_space(3))) i16x4 *;
+            const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)p));
+            const u32x2 c = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Read)(p + 4 * N * 2)));
+            return u32x4{a[0], a[1], c[0], c[1]};
+        } else {
+            static_assert(P::kSize == 4);
+            const lds_bytes p = from + 4 * (4 * h + s) * (N * 4) + (b * 32 + l % 32) * 4;
+            u32x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v[j] = *(const __attribute__((address_space(3))) uint32_t *)(p + j * (N * 4));
+            return v;
+        }
+    }
+};
+
+// ------------------------------------------------------------------- tiles --
+// Rows of expert e, whatever the offsets hold.
+__device__ __forceinline__ void expert_rows(const ProductParams &p, uint32_t e, uint32_t &lo, uint32_t &hi)
+{
+    const int32_t a = p.offsets[e], b = p.offsets[e + 1];
+    lo = a < 0 ? 0u : (uint32_t)a < p.rows ? (uint32_t)a : p.rows;
+    hi = b < (int32_t)lo ? lo : (uint32_t)b < p.rows ? (uint32_t)b : p.rows;
+}
+
+// Tiles of BM rows over all experts, in their order; a thread keeps a few experts.
+template <int THREADS>
+struct RowTiles {
+    static constexpr int kEach = XRED_MAX_EXPERTS / THREADS;
+    uint32_t lo[kEach], hi[kEach], first[kEach], tiles[kEach];
+    uint32_t total;
+
+    // shared: THREADS / 64 words.  Ends with a barrier.
+    __device__ __forceinline__ void start(const ProductParams &p, uint32_t rows_of_tile, uint32_t *shared)
+    {
+        uint32_t own = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const uint32_t e = threadIdx.x * kEach + j;
+            lo[j] = hi[j] = 0;
+            if (e < p.experts) expert_rows(p, e, lo[j], hi[j]);
+            tiles[j] = (hi[j] - lo[j] + rows_of_tile - 1) / rows_of_tile;
+            first[j] = own;
+            own += tiles[j];
+        }
+        uint32_t before, all;
+        lanes_before<64>(own, before, all);
+        if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = all;
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (uint32_t w = 0; w < THREADS / 64; ++w) {
+            before += w < threadIdx.x / 64 ? shared[w] : 0;
+            total += shared[w];
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) first[j] += before;
+    }
+
+    // Tile t (below total): its expert and rows [lo, hi), into found[3] (LDS).
+    __device__ __forceinline__ void find(uint32_t t, uint32_t rows_of_tile, uint32_t *found) const
+    {
+        __syncthreads();   // the tile before has been read
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (t - first[j] < tiles[j]) {
+                found[0] = threadIdx.x * kEach + j;
+                found[1] = lo[j] + (t - first[j]) * rows_of_tile;
+                found[2] = hi[j];
+            }
+        __syncthreads();
+    }
+};
+
+// Place i of a launch to a tile: workgroups i, i + 8, ... run on one XCD, and get
+// neighbouring tiles, whose operands its L2 then holds; false: none.
+__device__ __forceinline__ bool tile_of(uint32_t i, uint32_t total, uint32_t &tile)
+{
+    const uint32_t share = (total + 7) / 8;
+    tile = i % 8 * share + i / 8;
+    return i / 8 < share && tile < total;
+}
+
+// Four output values from column c on, n of them.
+__device__ __forceinline__ void store_four(char *row, uint32_t c, uint32_t n, const float (&v)[4],
+                                           xred_dtype type)
+{
+    if (type == XRED_FLOAT32) {
+        if (n == 4) {
+            *(__attribute__((address_space(1))) u32x4_any *)((global_out)row + c * 4ull) =
+                u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                      __float_as_uint(v[3])};
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+                if (j < n) down1<TF32, OpSum>(row, c + j, v[j]);
+        }
+        return;
+    }
+    u32x2 w;
+    if (type == XRED_BFLOAT16) {
+        w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[0], v[1]}, bf16x2));
+        w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2], v[3]}, bf16x2));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t a = __builtin_bit_cast(uint16_t, (_Float16)v[2 * j]);
+            const uint32_t b = __builtin_bit_cast(uint16_t, (_Float16)v[2 * j + 1]);
+            w[j] = a | b << 16;
+        }
+    }
+    if (n == 4) {
+        *(__attribute__((address_space(1))) u32x2_any *)((global_out)row + c * 2ull) = w;
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            if (j < n) ((uint16_t *)row)[c + j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+    }
+}
+
+__device__ __forceinline__ float value_at(const char *row, uint32_t c, xred_dtype type)
+{
+    return type == XRED_FLOAT32 ? up1<TF32>(row, c)
+         : type == XRED_BFLOAT16 ? up1<TBF16>(row, c) : up1<TF16>(row, c);
+}
+
+// ------------------------------------------------------------------ kernel --
+// 4 waves, two by two, each RB x CB blocks of 32 x 32: tiles of 64 RB x 64 CB.
+template <class P, bool GRAD, bool ACROSS, bool DIRECT, int RB, int CB>
+__global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams p)
+{
+    constexpr int BM = 64 * RB, BN = 64 * CB;
+    using Rows = Operand<P, GRAD, DIRECT, BM>;
+    using Columns = Operand<P, ACROSS, DIRECT, BN>;
+    // two steps, each an array of its own: a read of one does not wait for loads into
+    // the other
+    __shared__ __attribute__((aligned(1024))) char rows0[BM * 128], rows1[BM * 128];
+    __shared__ __attribute__((aligned(1024))) char columns0[BN * 128], columns1[BN * 128];
+    __shared__ uint32_t shared[kProductThreads / 64], found[3];
+    const uint32_t l = threadIdx.x % 64, h = l / 32;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t wr = wave / 2, wc = wave % 2;   // this wave's place
+    RowTiles<kProductThreads> all;
+    uint32_t total;
+    if constexpr (GRAD) {
+        total = p.experts * p.row_tiles * p.col_tiles;
+    } else {
+        all.start(p, BM, shared);
+        total = all.total * p.col_tiles;
+    }
+    for (uint32_t i = blockIdx.x; i / 8 < (total + 7) / 8; i += gridDim.x) {
+        uint32_t tile;
+        if (!tile_of(i, total, tile)) continue;
+        uint32_t e, m0, n0, items, length;   // expert; first row, column; rows; of k
+        const char *from, *col_from;
+        if constexpr (GRAD) {
+            e = tile / (p.row_tiles * p.col_tiles);
+            const uint32_t rest = tile - e * p.row_tiles * p.col_tiles;
+            m0 = rest % p.row_tiles * BM;
+            n0 = rest / p.row_tiles * BN;
+            uint32_t lo, hi;
+            expert_rows(p, e, lo, hi);
+            length = hi - lo;
+            items = p.m - m0;
+            from = p.row + lo * p.row_stride + (uint64_t)m0 * P::kSize;
+            col_from = p.col + lo * p.col_stride + (uint64_t)n0 * P::kSize;
+        } else {
+            // groups of four row tiles, column by column
+            const uint32_t group = tile / (4 * p.col_tiles), rest = tile - group * 4 * p.col_tiles;
+            const uint32_t left = all.total - group * 4, high = left < 4 ? left : 4;
+            all.find(group * 4 + rest % high, BM, found);
+            e = found[0];
+            m0 = found[1];
+            items = found[2] - m0;
+            n0 = rest / high * BN;
+            length = p.k * P::kSize;
+            from = p.row + m0 * p.row_stride;
+            col_from = p.col + e * p.col_expert + n0 * (ACROSS ? (uint64_t)P::kSize : p.col_stride);
+        }
+        Rows rows;
+        Columns columns;
+        rows.start(from, p.row_stride, items);
+        columns.start(col_from, p.col_stride, p.n - n0);
+        f32x16 acc[RB][CB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) acc[r][c] = f32x16{};
+
+        const uint32_t per = GRAD ? Rows::kRows : 128;
+        const uint32_t steps = (length + per - 1) / per;
+        // across operands count k in rows
+        const uint32_t col_length = ACROSS && !GRAD ? p.k : length;
+        // where this lane's rows and columns have their scales
+        const char *rs[RB], *cs[CB];
+        if constexpr (__is_same(P, PE4M3) || __is_same(P, PMx4)) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const uint32_t row = (wr * RB + r) * 32 + l % 32;
+                rs[r] = p.row_scale + (m0 + (row < items ? row : items - 1)) * p.row_scale_stride;
+            }
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                uint32_t col = n0 + (wc * CB + c) * 32 + (__is_same(P, PMx4) ? l % 32 : 0);
+                col = col < p.n ? col : p.n - 1;
+                cs[c] = p.col_scale + e * p.col_scale_expert +
+                        (__is_same(P, PMx4) ? col : col / 128) * p.col_scale_stride;
+            }
+        }
+        auto multiply_step = [&](uint32_t t, lds_bytes row_step, lds_bytes column_step) {
+            if constexpr (__is_same(P, PE4M3)) {
+                u32x4 rf[4][RB], cf[4][CB];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) rf[s][r] = Rows::fragment(row_step, wr * RB + r, s);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c)
+                        cf[s][c] = Columns::fragment(column_step, wc * CB + c, s);
+                }
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const float a = *(const float *)(rs[r] + t * 4ull);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) {
+                        const float by = a * *(const float *)(cs[c] + t * 4ull);
+                        f32x16 part = multiply_e4m3(cf[0][c], cf[1][c], rf[0][r], rf[1][r], f32x16{});
+                        part = multiply_e4m3(cf[2][c], cf[3][c], rf[2][r], rf[3][r], part);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            acc[r][c][j] = __builtin_fmaf(part[j], by, acc[r][c][j]);
+                    }
+                }
+            } else {
+                uint32_t re[RB], ce[CB];   // mx4: four exponents each
+                if constexpr (__is_same(P, PMx4)) {
+                    const uint32_t at = t * 8 + 4 * h, count = p.k / 16;
+                    auto exponents = [&](const char *from) {
+                        if (at + 4 <= count)
+                            return *(const __attribute__((address_space(1))) u32_any *)((global_bytes)from + at);
+                        uint32_t v = 0;
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; ++j)
+                            if (at + j < count) v |= (uint32_t)(uint8_t)from[at + j] << (8 * j);
+                        return v;
+                    };
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) re[r] = exponents(rs[r]);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) ce[c] = exponents(cs[c]);
+                }
+                auto sub_step = [&](auto sub) {
+                    constexpr int S = decltype(sub)::value;
+                    u32x4 rf[RB], cf[CB];
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) rf[r] = Rows::fragment(row_step, wr * RB + r, S);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) cf[c] = Columns::fragment(column_step, wc * CB + c, S);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+#pragma unroll
+                        for (int c = 0; c < CB; ++c) {
+                            if constexpr (__is_same(P, PMx4))
+                                acc[r][c] = multiply_mx4<S>(cf[c], rf[r], ce[c], re[r], acc[r][c]);
+                            else
+                                acc[r][c] = multiply<P>(cf[c], rf[r], acc[r][c]);
+                        }
+                };
+                sub_step(std::integral_constant<int, 0>{});
+                sub_step(std::integral_constant<int, 1>{});
+                sub_step(std::integral_constant<int, 2>{});
+                sub_step(std::integral_constant<int, 3>{});
+            }
+        };
+        const lds_bytes r0 = (lds_bytes)rows0, r1 = (lds_bytes)rows1;
+        const lds_bytes c0 = (lds_bytes)columns0, c1 = (lds_bytes)columns1;
+        // a step's loads are on their way while the step before is multiplied
+        auto step = [&](uint32_t t, lds_bytes rn, lds_bytes cn, lds_bytes rt, lds_bytes ct) {
+            if (t + 1 < steps) {
+                rows.load(t + 1, length, rn);
+                columns.load(t + 1, col_length, cn);
+            }
+            multiply_step(t, rt, ct);
+            if (t + 1 < steps) {
+                rows.store(rn);
+                columns.store(cn);
+            }
+            __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+        };
+        if (steps) {
+            rows.load(0, length, r0);
+            columns.load(0, col_length, c0);
+            rows.store(r0);
+            columns.store(c0);
+            __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            for (uint32_t t = 0; t < steps; t += 2) {
+                step(t, r1, c1, r0, c0);
+                if (t + 1 < steps) step(t + 1, r0, c0, r1, c1);
+            }
+        }
+        char *out = p.out + (GRAD ? e * p.out_expert : 0) + m0 * p.out_stride;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const uint32_t row = (wr * RB + r) * 32 + l % 32;
+            if (row < items) {
+                char *to = out + row * p.out_stride;
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t col = n0 + (wc * CB + c) * 32 + 8 * q + 4 * h;
+                        if (col < p.n) {
+                            const uint32_t n = p.n - col < 4 ? p.n - col : 4;
+                            float v[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) v[j] = acc[r][c][4 * q + j];
+                            if (GRAD && p.add)
+#pragma unroll
+                                for (uint32_t j = 0; j < 4; ++j)
+                                    if (j < n) v[j] += value_at(to, col + j, p.out_type);
+                            store_four(to, col, n, v, p.out_type);
+                        }
+                    }
+            }
+        }
+    }
+}
+
+template <class P, bool GRAD, bool ACROSS, bool DIRECT, int RB, int CB>
+hipError_t go_product(ProductParams p, hipStream_t s)
+{
+    constexpr uint32_t BM = 64 * RB, BN = 64 * CB;
+    p.col_tiles = (p.n + BN - 1) / BN;
+    p.row_tiles = (p.m + BM - 1) / BM;
+    // forward: every expert may end in a tile that is not whole
+    const uint64_t tiles = GRAD ? (uint64_t)p.experts * p.row_tiles
+                                : p.rows / BM + (p.rows < p.experts ? p.rows : p.experts);
+    return launch_kernel(product_kernel<P, GRAD, ACROSS, DIRECT, RB, CB>,
+                         dim3(grid_of((tiles * p.col_tiles + 7) / 8 * 8, kProductThreads)),
+                         dim3(kProductThreads), 0, s, p);
+}
+
+// Whether an operand's 16-byte pieces lie on the 16-byte grid, whole ones only, so that
+// loads can go straight to LDS.
+inline bool on_grid(const char *base, uint64_t stride, uint64_t apart, uint64_t width)
+{
+    return ((uintptr_t)base | stride | apart | width) % 16 == 0;
+}
+
+template <class P>
+hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, hipStream_t s)
+{
+    constexpr uint64_t es = P::kSize;
+    if (grad) {
+        const bool direct = on_grid(p.row, p.row_stride, 0, p.m * es) &&
+                            on_grid(p.col, p.col_stride, 0, p.n * es);
+        return direct ? go_product<P, true, true, true, 2, 2>(p, s)
+                      : go_product<P, true, true, false, 2, 2>(p, s);
+    }
+    const bool direct = on_grid(p.row, p.row_stride, 0, p.k * es) &&
+                        on_grid(p.col, p.col_stride, p.col_expert, (across ? p.n : p.k) * es);
+    if (across)
+        return direct ? go_product<P, false, true, true, 2, 2>(p, s)
+                      : go_product<P, false, true, false, 2, 2>(p, s);
+    return direct ? go_product<P, false, false, true, 2, 2>(p, s)
+                  : go_product<P, false, false, false, 2, 2>(p, s);
+}
+
+template <class P>
+hipError_t launch_product_scaled(const ProductParams &p, hipStream_t s)
+{
+    const bool direct = on_grid(p.row, p.row_stride, 0, p.k) &&
+                        on_grid(p.col, p.col_stride, p.col_expert, p.k);
+    return direct ? go_product<P, false, false, true, 2, 2>(p, s)
+                  : go_product<P, false, false, false, 2, 2>(p, s);
+}
+
+}  // namespace xred

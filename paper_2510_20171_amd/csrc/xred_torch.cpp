@@ -43,6 +43,12 @@ decltype(&xred_dispatch_plan_workspace) f_dispatch_plan_workspace;
 decltype(&xred_dispatch) f_dispatch;
 decltype(&xred_combine) f_combine;
 decltype(&xred_combine_grad) f_combine_grad;
+decltype(&xred_group_product) f_group_product;
+decltype(&xred_group_product_grad) f_group_product_grad;
+decltype(&xred_gate) f_gate;
+decltype(&xred_gate_grad) f_gate_grad;
+decltype(&xred_quant_mx4) f_quant_mx4;
+decltype(&xred_dequant_mx4) f_dequant_mx4;
 PyObject *current_raw_stream;
 
 // Raised to leave a call to the Python code.
@@ -695,6 +701,192 @@ PyObject *combine_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
+// ------------------------------------------------ between dispatch and combine --
+// The experts' matrices, each rows x columns: the first one, and the elements from one
+// to the next.
+xred_rows stack_of(PyObject *o, c10::Device dev, int64_t experts, int64_t rows, int64_t columns,
+                   at::ScalarType type, uint64_t *apart)
+{
+    const at::Tensor &t = tensor(o);
+    if (!t.is_cuda() || t.device() != dev || t.scalar_type() != type || t.dim() != 3 ||
+        t.size(0) != experts || t.size(1) != rows || t.size(2) != columns ||
+        (columns > 1 && t.stride(2) != 1) || (rows > 1 && t.stride(1) < columns))
+        throw Decline{};
+    const int64_t stride = rows > 1 ? t.stride(1) : columns;
+    *apart = (uint64_t)(experts > 1 ? t.stride(0) : rows * stride);
+    return {t.data_ptr(), (uint64_t)stride};
+}
+
+const int32_t *offsets_of(PyObject *o, c10::Device dev, uint32_t *experts)
+{
+    const at::Tensor &t = tensor(o);
+    if (t.dim() != 1 || t.numel() < 2 || t.numel() > XRED_MAX_EXPERTS + 1) throw Decline{};
+    *experts = (uint32_t)t.numel() - 1;
+    return (const int32_t *)vector(o, dev, t.numel(), at::kInt);
+}
+
+bool flag_of(PyObject *o)
+{
+    if (o != Py_True && o != Py_False) throw Decline{};
+    return o == Py_True;
+}
+
+// An output's matrix of fp32, bf16 or fp16.
+xred_rows typed_rows(PyObject *o, const Matrix &m, xred_dtype *dtype)
+{
+    const Matrix to = lead(o, dtype);
+    if (to.dev != m.dev || to.rows != m.rows || to.columns != m.columns) throw Decline{};
+    return m(o, m.columns, to.type);
+}
+
+// group_product(x, w, offsets, out, scale, w_scale, transpose, stream)
+PyObject *group_product(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 8, [&] {
+        xred_group_product_args n{};
+        const Matrix m = lead(a[0], &n.dtype, true);
+        const int64_t columns = slots_per_token(a[3]);
+        const bool mx4 = n.dtype == XRED_UINT8, scaled = mx4 || n.dtype == XRED_FP8_E4M3;
+        const bool across = flag_of(a[6]);
+        if (!scaled && n.dtype != XRED_FLOAT32 && n.dtype != XRED_BFLOAT16 &&
+            n.dtype != XRED_FLOAT16)
+            throw Decline{};
+        if (scaled != (a[4] != Py_None) || scaled != (a[5] != Py_None) || (mx4 && m.columns % 16))
+            throw Decline{};
+        n.rows = (uint64_t)m.rows;
+        n.n = (uint64_t)columns;
+        n.k = (uint64_t)(mx4 ? 2 * m.columns : m.columns);
+        n.flags = (across ? XRED_PRODUCT_TRANSPOSE : 0u) | (mx4 ? XRED_PRODUCT_MX4 : 0u);
+        n.offsets = offsets_of(a[2], m.dev, &n.experts);
+        n.x = m(a[0]);
+        n.out = typed_rows(a[3], Matrix{m.dev, m.rows, columns, m.type}, &n.out_dtype);
+        if (!scaled && n.out_dtype != n.dtype && n.out_dtype != XRED_FLOAT32) throw Decline{};
+        n.w = across ? stack_of(a[1], m.dev, n.experts, m.columns, columns, m.type, &n.w_expert)
+                     : stack_of(a[1], m.dev, n.experts, columns, m.columns, m.type, &n.w_expert);
+        if (scaled) {
+            const at::ScalarType t = mx4 ? at::kByte : at::kFloat;
+            const int64_t parts = mx4 ? m.columns / 16 : (m.columns + 127) / 128;
+            n.scale = m(a[4], parts, t);
+            n.w_scale = stack_of(a[5], m.dev, n.experts, mx4 ? columns : (columns + 127) / 128, parts,
+                                 t, &n.w_scale_expert);
+        }
+        void *stream = stream_of(a[7], m.dev);
+        return unlocked([&] { return f_group_product(&n, stream); });
+    });
+}
+
+// group_product_grad(dout, x, offsets, dw, add, stream)
+PyObject *group_product_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 6, [&] {
+        xred_group_product_grad_args n{};
+        const Matrix m = lead(a[0], &n.dtype);
+        const int64_t k = slots_per_token(a[1]);
+        n.rows = (uint64_t)m.rows;
+        n.n = (uint64_t)m.columns;
+        n.k = (uint64_t)k;
+        n.flags = flag_of(a[4]) ? XRED_PRODUCT_ADD : 0u;
+        n.offsets = offsets_of(a[2], m.dev, &n.experts);
+        n.dout = m(a[0]);
+        if (a[1] == Py_None) throw Decline{};
+        n.x = m(a[1], k, m.type);
+        const at::ScalarType to = tensor(a[3]).scalar_type();
+        if (to != m.type && to != at::kFloat) throw Decline{};
+        n.dw_dtype = to == m.type ? n.dtype : XRED_FLOAT32;
+        n.dw = stack_of(a[3], m.dev, n.experts, m.columns, k, to, &n.dw_expert);
+        void *stream = stream_of(a[5], m.dev);
+        return unlocked([&] { return f_group_product_grad(&n, stream); });
+    });
+}
+
+// The last of offsets, or None.
+const int32_t *row_count(PyObject *o, c10::Device dev)
+{
+    if (o == Py_None) return nullptr;
+    const int64_t n = tensor(o).numel();
+    if (n < 1) throw Decline{};
+    return (const int32_t *)vector(o, dev, n, at::kInt) + n - 1;
+}
+
+// gate(x, out, out8, scale, group, offsets, stream)
+PyObject *gate(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 7, [&] {
+        xred_gate_args n{};
+        const Matrix m = lead(a[0], &n.dtype);
+        if (m.columns % 2) throw Decline{};
+        const int64_t width = m.columns / 2;
+        n.rows = (uint64_t)m.rows;
+        n.width = (uint64_t)width;
+        n.group = u32_of(a[4]);
+        n.x = m(a[0]);
+        n.out = m(a[1], width, m.type);
+        if (a[2] != Py_None) {
+            const at::ScalarType t = tensor(a[2]).scalar_type();
+            if (t != at::kFloat8_e4m3fn && t != at::kByte) throw Decline{};
+            n.out8 = m(a[2], width, t);
+        }
+        n.scale = m(a[3], n.group ? (width + n.group - 1) / n.group : 1, at::kFloat);
+        n.count = row_count(a[5], m.dev);
+        void *stream = stream_of(a[6], m.dev);
+        return unlocked([&] { return f_gate(&n, stream); });
+    });
+}
+
+// gate_grad(dout, x, dx, offsets, stream)
+PyObject *gate_grad(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 5, [&] {
+        xred_gate_grad_args n{};
+        const Matrix m = lead(a[0], &n.dtype);
+        if (a[1] == Py_None || a[2] == Py_None) throw Decline{};
+        n.rows = (uint64_t)m.rows;
+        n.width = (uint64_t)m.columns;
+        n.dout = m(a[0]);
+        n.x = m(a[1], 2 * m.columns, m.type);
+        n.dx = m(a[2], 2 * m.columns, m.type);
+        n.count = row_count(a[3], m.dev);
+        void *stream = stream_of(a[4], m.dev);
+        return unlocked([&] { return f_gate_grad(&n, stream); });
+    });
+}
+
+// quant_mx4(x, out4, scale, stream)
+PyObject *quant_mx4(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 4, [&] {
+        xred_quant_mx4_args n{};
+        const Matrix m = lead(a[0], &n.dtype);
+        if (a[1] == Py_None || a[2] == Py_None) throw Decline{};
+        const int64_t blocks = (m.columns + 31) / 32;
+        n.rows = (uint64_t)m.rows;
+        n.columns = (uint64_t)m.columns;
+        n.x = m(a[0]);
+        n.out4 = m(a[1], 16 * blocks, at::kByte);
+        n.scale = m(a[2], blocks, at::kByte);
+        void *stream = stream_of(a[3], m.dev);
+        return unlocked([&] { return f_quant_mx4(&n, stream); });
+    });
+}
+
+// dequant_mx4(x4, scale, out, stream)
+PyObject *dequant_mx4(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return entry(nargs, 4, [&] {
+        xred_dequant_mx4_args n{};
+        const Matrix m = lead(a[2], &n.dtype);
+        if (a[0] == Py_None || a[1] == Py_None) throw Decline{};
+        const int64_t blocks = (m.columns + 31) / 32;
+        n.rows = (uint64_t)m.rows;
+        n.columns = (uint64_t)m.columns;
+        n.x4 = m(a[0], 16 * blocks, at::kByte);
+        n.scale = m(a[1], blocks, at::kByte);
+        n.out = m(a[2]);
+        void *stream = stream_of(a[3], m.dev);
+        return unlocked([&] { return f_dequant_mx4(&n, stream); });
+    });
+}
+
 // bind(current_raw_stream, {name: address}): once, by the loader.
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -719,6 +911,10 @@ PyObject *bind(PyObject *, PyObject *args)
         !take("xred_dispatch_plan_workspace", f_dispatch_plan_workspace) ||
         !take("xred_dispatch", f_dispatch) || !take("xred_combine", f_combine) ||
         !take("xred_combine_grad", f_combine_grad) ||
+        !take("xred_group_product", f_group_product) ||
+        !take("xred_group_product_grad", f_group_product_grad) || !take("xred_gate", f_gate) ||
+        !take("xred_gate_grad", f_gate_grad) || !take("xred_quant_mx4", f_quant_mx4) ||
+        !take("xred_dequant_mx4", f_dequant_mx4) ||
         !take("xred_allreduce_local", all))
         return nullptr;
     Py_INCREF(get);
@@ -744,6 +940,12 @@ PyMethodDef methods[] = {
     {"dispatch", (PyCFunction)(void *)dispatch, METH_FASTCALL, nullptr},
     {"combine", (PyCFunction)(void *)combine, METH_FASTCALL, nullptr},
     {"combine_grad", (PyCFunction)(void *)combine_grad, METH_FASTCALL, nullptr},
+    {"group_product", (PyCFunction)(void *)group_product, METH_FASTCALL, nullptr},
+    {"group_product_grad", (PyCFunction)(void *)group_product_grad, METH_FASTCALL, nullptr},
+    {"gate", (PyCFunction)(void *)gate, METH_FASTCALL, nullptr},
+    {"gate_grad", (PyCFunction)(void *)gate_grad, METH_FASTCALL, nullptr},
+    {"quant_mx4", (PyCFunction)(void *)quant_mx4, METH_FASTCALL, nullptr},
+    {"dequant_mx4", (PyCFunction)(void *)dequant_mx4, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_xred_torch",
