@@ -49,6 +49,12 @@ struct PMx4 {
     static constexpr int kSize = 1, kStep = 128;   // counted in bytes
 };
 
+// The element type of an unscaled operand, as an output's.
+template <class P> struct OwnType;
+template <> struct OwnType<PBF16> { using T = TBF16; };
+template <> struct OwnType<PF16> { using T = TF16; };
+template <> struct OwnType<PF32> { using T = TF32; };
+
 constexpr int kProductThreads = 256;
 
 // acc += columns' fragment (32 columns) * rows' fragment (32 rows): lane l has row
@@ -191,9 +197,10 @@ struct Operand {
     }
 
     // Sub-step s of block b of 32.
-    static __device__ __forceinline__ u32x4 fragment(lds_bytes from, int b, int s)
+    static __device__ __forceinline__ u32x4 fragment(lds_bytes from, int b, int s,
+                                                     uint32_t l = threadIdx.x % 64)
     {
-        const uint32_t l = threadIdx.x % 64, h = l / 32;
+        const uint32_t h = l / 32;
         if constexpr (!ACROSS) {
             return *(const __attribute__((address_space(3))) u32x4 *)(
                 from + b * 4096 + l % 32 * 128 + ((4 * h + s) ^ l % 8) * 16);
@@ -235,8 +242,10 @@ struct RowTiles {
     uint32_t lo[kEach], hi[kEach], first[kEach], tiles[kEach];
     uint32_t total;
 
-    // shared: THREADS / 64 words.  Ends with a barrier.
-    __device__ __forceinline__ void start(const ProductParams &p, uint32_t rows_of_tile, uint32_t *shared)
+    // tiles_of(n): of an expert with n rows.  shared: THREADS / 64 words.  Ends with a
+    // barrier.
+    template <class F>
+    __device__ __forceinline__ void start(const ProductParams &p, uint32_t *shared, F &&tiles_of)
     {
         uint32_t own = 0;
 #pragma unroll
@@ -244,7 +253,7 @@ struct RowTiles {
             const uint32_t e = threadIdx.x * kEach + j;
             lo[j] = hi[j] = 0;
             if (e < p.experts) expert_rows(p, e, lo[j], hi[j]);
-            tiles[j] = (hi[j] - lo[j] + rows_of_tile - 1) / rows_of_tile;
+            tiles[j] = tiles_of(hi[j] - lo[j]);
             first[j] = own;
             own += tiles[j];
         }
@@ -286,6 +295,15 @@ __device__ __forceinline__ bool tile_of(uint32_t i, uint32_t total, uint32_t &ti
     return i / 8 < share && tile < total;
 }
 
+// Two values of bf16 or fp16 as a word.
+__device__ __forceinline__ uint32_t pair_of(float a, float b, xred_dtype type)
+{
+    if (type == XRED_BFLOAT16)
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
+    const uint32_t lo = __builtin_bit_cast(uint16_t, (_Float16)a);
+    return lo | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
+}
+
 // Four output values from column c on, n of them.
 __device__ __forceinline__ void store_four(char *row, uint32_t c, uint32_t n, const float (&v)[4],
                                            xred_dtype type)
@@ -302,18 +320,7 @@ __device__ __forceinline__ void store_four(char *row, uint32_t c, uint32_t n, co
         }
         return;
     }
-    u32x2 w;
-    if (type == XRED_BFLOAT16) {
-        w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[0], v[1]}, bf16x2));
-        w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2], v[3]}, bf16x2));
-    } else {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t a = __builtin_bit_cast(uint16_t, (_Float16)v[2 * j]);
-            const uint32_t b = __builtin_bit_cast(uint16_t, (_Float16)v[2 * j + 1]);
-            w[j] = a | b << 16;
-        }
-    }
+    const u32x2 w = {pair_of(v[0], v[1], type), pair_of(v[2], v[3], type)};
     if (n == 4) {
         *(__attribute__((address_space(1))) u32x2_any *)((global_out)row + c * 2ull) = w;
     } else {
@@ -350,7 +357,7 @@ __global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams 
     if constexpr (GRAD) {
         total = p.experts * p.row_tiles * p.col_tiles;
     } else {
-        all.start(p, BM, shared);
+        all.start(p, shared, [](uint32_t n) { return (n + BM - 1) / BM; });
         total = all.total * p.col_tiles;
     }
     for (uint32_t i = blockIdx.x; i / 8 < (total + 7) / 8; i += gridDim.x) {
@@ -552,34 +559,6 @@ hipError_t go_product(ProductParams p, hipStream_t s)
 inline bool on_grid(const char *base, uint64_t stride, uint64_t apart, uint64_t width)
 {
     return ((uintptr_t)base | stride | apart | width) % 16 == 0;
-}
-
-template <class P>
-hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, hipStream_t s)
-{
-    constexpr uint64_t es = P::kSize;
-    if (grad) {
-        const bool direct = on_grid(p.row, p.row_stride, 0, p.m * es) &&
-                            on_grid(p.col, p.col_stride, 0, p.n * es);
-        return direct ? go_product<P, true, true, true, 2, 2>(p, s)
-                      : go_product<P, true, true, false, 2, 2>(p, s);
-    }
-    const bool direct = on_grid(p.row, p.row_stride, 0, p.k * es) &&
-                        on_grid(p.col, p.col_stride, p.col_expert, (across ? p.n : p.k) * es);
-    if (across)
-        return direct ? go_product<P, false, true, true, 2, 2>(p, s)
-                      : go_product<P, false, true, false, 2, 2>(p, s);
-    return direct ? go_product<P, false, false, true, 2, 2>(p, s)
-                  : go_product<P, false, false, false, 2, 2>(p, s);
-}
-
-template <class P>
-hipError_t launch_product_scaled(const ProductParams &p, hipStream_t s)
-{
-    const bool direct = on_grid(p.row, p.row_stride, 0, p.k) &&
-                        on_grid(p.col, p.col_stride, p.col_expert, p.k);
-    return direct ? go_product<P, false, false, true, 2, 2>(p, s)
-                  : go_product<P, false, false, false, 2, 2>(p, s);
 }
 
 }  // namespace xred

@@ -1,5 +1,5 @@
 // xred_product_bf16.hip -- the experts' products in bf16.
-#include "xred_product.hpp"
+#include "xred_product_choice.hpp"
 
 namespace xred {
 

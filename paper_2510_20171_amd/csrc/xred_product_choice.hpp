@@ -1,0 +1,49 @@
+// xred_product_choice.hpp -- which kernel takes a product, by types, sizes and alignment.
+#pragma once
+
+#include "xred_product_wide.hpp"
+
+namespace xred {
+
+// Tiles of 256 x 256 fill the chip from about half a tile a CU on.
+inline bool wide_pays(const ProductParams &p, bool grad)
+{
+    const uint64_t columns = (p.n + 255) / 256;
+    const uint64_t rows = grad ? (uint64_t)p.experts * ((p.m + 255) / 256)
+                               : p.rows / 256 + (p.rows < p.experts ? p.rows : p.experts);
+    return p.n > 128 && rows * columns >= 128;
+}
+
+template <class P>
+hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, hipStream_t s)
+{
+    constexpr uint64_t es = P::kSize;
+    const bool direct = grad ? on_grid(p.row, p.row_stride, 0, p.m * es) &&
+                                   on_grid(p.col, p.col_stride, 0, p.n * es)
+                             : on_grid(p.row, p.row_stride, 0, p.k * es) &&
+                                   on_grid(p.col, p.col_stride, p.col_expert, (across ? p.n : p.k) * es);
+    if (direct && p.row_stride < kWideStride && p.col_stride < kWideStride && wide_pays(p, grad)) {
+        return p.out_type == XRED_FLOAT32
+                   ? launch_wide<P, TF32>(p, grad, across, s)
+                   : launch_wide<P, typename OwnType<P>::T>(p, grad, across, s);
+    }
+    if (grad)
+        return direct ? go_product<P, true, true, true, 2, 2>(p, s)
+                      : go_product<P, true, true, false, 2, 2>(p, s);
+    if (across)
+        return direct ? go_product<P, false, true, true, 2, 2>(p, s)
+                      : go_product<P, false, true, false, 2, 2>(p, s);
+    return direct ? go_product<P, false, false, true, 2, 2>(p, s)
+                  : go_product<P, false, false, false, 2, 2>(p, s);
+}
+
+template <class P>
+hipError_t launch_product_scaled(const ProductParams &p, hipStream_t s)
+{
+    const bool direct = on_grid(p.row, p.row_stride, 0, p.k) &&
+                        on_grid(p.col, p.col_stride, p.col_expert, p.k);
+    return direct ? go_product<P, false, false, true, 2, 2>(p, s)
+                  : go_product<P, false, false, false, 2, 2>(p, s);
+}
+
+}  // namespace xred

@@ -1,5 +1,5 @@
 // xred_product_e4m3.hip -- the experts' products in e4m3 with scales by 128 elements.
-#include "xred_product.hpp"
+#include "xred_product_choice.hpp"
 
 namespace xred {
 

@@ -1,5 +1,5 @@
 // xred_product_f16.hip -- the experts' products in f16.
-#include "xred_product.hpp"
+#include "xred_product_choice.hpp"
 
 namespace xred {
 

@@ -1,5 +1,5 @@
 // xred_product_f32.hip -- the experts' products in f32.
-#include "xred_product.hpp"
+#include "xred_product_choice.hpp"
 
 namespace xred {
 

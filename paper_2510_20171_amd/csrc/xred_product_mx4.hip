@@ -1,5 +1,5 @@
 // xred_product_mx4.hip -- the experts' products in mx4 (e2m1 with exponents by 32).
-#include "xred_product.hpp"
+#include "xred_product_choice.hpp"
 
 namespace xred {
 
