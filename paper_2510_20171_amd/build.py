@@ -50,6 +50,10 @@ HIPFLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
+# and of single files: sums in e4m3 are scaled by vector instructions, so matrix
+# instructions have to leave them where those read
+FLAGS_OF = {"xred_product_e4m3": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 def _run(cmd):
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -87,7 +91,8 @@ def build(jobs: int = 0, verbose: bool = False) -> Path:
     BUILD.mkdir(exist_ok=True)
     sources = sorted(CSRC.glob("*.hip"))
     objs = [BUILD / (s.stem + ".o") for s in sources]
-    cmds = [[HIPCC, *HIPFLAGS, "-c", str(s), "-o", str(o)] for s, o in zip(sources, objs)]
+    cmds = [[HIPCC, *HIPFLAGS, *FLAGS_OF.get(s.stem, []), "-c", str(s), "-o", str(o)]
+            for s, o in zip(sources, objs)]
     ceiling_tmp = CEILING_OUT.with_suffix(".so.tmp")
     cmds.append([HIPCC, *HIPFLAGS, "-shared", str(CEILING_SRC), "-o", str(ceiling_tmp)])
     torch_tmp = TORCH_OUT.with_suffix(".so.tmp")

@@ -37,11 +37,26 @@ hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, 
                   : go_product<P, false, false, false, 2, 2>(p, s);
 }
 
+// Whether scales can be read by whole words (mx4: its exponents, four of them).
+template <class P>
+inline bool scale_words(const ProductParams &p)
+{
+    return (__is_same(P, PE4M3) ||
+            ((uintptr_t)p.row_scale | p.row_scale_stride | (uintptr_t)p.col_scale | p.col_scale_stride |
+             p.col_scale_expert | p.k / 16) % 4 == 0) &&
+           p.row_scale_stride < kWideStride && p.col_scale_stride < kWideStride;
+}
+
 template <class P>
 hipError_t launch_product_scaled(const ProductParams &p, hipStream_t s)
 {
     const bool direct = on_grid(p.row, p.row_stride, 0, p.k) &&
                         on_grid(p.col, p.col_stride, p.col_expert, p.k);
+    if (direct && p.row_stride < kWideStride && p.col_stride < kWideStride && scale_words<P>(p) &&
+        wide_pays(p, false))
+        return p.out_type == XRED_FLOAT32    ? launch_wide<P, TF32>(p, false, false, s)
+               : p.out_type == XRED_BFLOAT16 ? launch_wide<P, TBF16>(p, false, false, s)
+                                             : launch_wide<P, TF16>(p, false, false, s);
     return direct ? go_product<P, false, false, true, 2, 2>(p, s)
                   : go_product<P, false, false, false, 2, 2>(p, s);
 }

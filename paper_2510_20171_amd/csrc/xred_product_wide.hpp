@@ -41,11 +41,11 @@ __device__ __forceinline__ void interleave()
     }
 }
 
-// 256 rows (along) or columns (across) of an operand, a tile's.
-template <class P, bool ACROSS>
+// N rows (along) or columns (across) of an operand, a tile's.
+template <class P, bool ACROSS, int N>
 struct WideOperand {
-    static constexpr int kPieces = 8;                  // of a thread and step
-    static constexpr int kWide = 256 * P::kSize / 16;  // across: pieces of a row of k
+    static constexpr int kPieces = N / 32;             // of a thread and step
+    static constexpr int kWide = N * P::kSize / 16;    // across: pieces of a row of k
     static constexpr int kRows = 128 / P::kSize;       // across: rows of k in a step
     static constexpr int kReads = ACROSS ? (P::kSize == 2 ? 2 : 4) : 1;   // of a fragment
 
@@ -61,7 +61,7 @@ struct WideOperand {
         base = from;
         step = ACROSS ? stride * kRows : 128;
         bytes = ACROSS ? (length - 1) * stride + (uint64_t)items * P::kSize
-                       : (uint64_t)(items < 256 ? items - 1 : 255) * stride + length;
+                       : (uint64_t)(items < N ? items - 1 : N - 1) * stride + length;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const uint32_t q = (tid / 64 * kPieces + i) * 64 + tid % 64;
@@ -123,7 +123,7 @@ struct WideOperand {
 
     static __device__ __forceinline__ u32x4 fragment(lds_bytes from, int b, int s, uint32_t lane)
     {
-        return Operand<P, ACROSS, true, 256>::fragment(from, b, s, lane);
+        return Operand<P, ACROSS, true, N>::fragment(from, b, s, lane);
     }
 };
 
@@ -151,21 +151,36 @@ __device__ __forceinline__ void uniform_rows(const ProductParams &p, uint32_t e,
     hi = __builtin_amdgcn_readfirstlane(hi);
 }
 
+// Columns of a tile.  e4m3's sums are scaled by vector instructions, which cannot reach
+// the accumulation registers: half as many fit beside what else a wave holds.
+template <class P>
+constexpr int wide_columns() { return __is_same(P, PE4M3) ? 128 : 256; }
+
 // O: the output's type.  ADD: onto what it holds (gradient).
 template <class P, class O, bool GRAD, bool ACROSS, bool ADD>
-__global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(ProductParams p)
+__device__ __forceinline__ void product_wide(const ProductParams &p)
 {
-    using Rows = WideOperand<P, GRAD>;
-    using Columns = WideOperand<P, ACROSS>;
-    constexpr bool kMx4 = __is_same(P, PMx4);
+    constexpr int BN = wide_columns<P>();
+    using Rows = WideOperand<P, GRAD, 256>;
+    using Columns = WideOperand<P, ACROSS, BN>;
+    constexpr bool kMx4 = __is_same(P, PMx4), kE4M3 = __is_same(P, PE4M3), kScaled = kMx4 || kE4M3;
+    constexpr int kThreads = kProductThreads, kWaves = kThreads / 64;
+    constexpr int CB = BN / 64, kAcross = 2;   // a wave's blocks of columns, waves side by side
     __shared__ __attribute__((aligned(1024))) char rows0[32768], rows1[32768];
-    __shared__ __attribute__((aligned(1024))) char columns0[32768], columns1[32768];
-    constexpr int kStage = 32 * 144;   // results of a wave on their way out
-    __shared__ __attribute__((aligned(16))) char stage[4 * kStage];
+    __shared__ __attribute__((aligned(1024))) char columns0[BN * 128], columns1[BN * 128];
+    // results of a wave on their way out: 32 rows of kChunk bytes, kPitch apart
+    constexpr int kChunk = kMx4 ? 64 : 128, kPitch = kChunk + 16, kStage = 32 * kPitch;
+    __shared__ __attribute__((aligned(1024))) char rows2[kE4M3 ? 32768 : kWaves * kStage];
+    __shared__ __attribute__((aligned(1024))) char columns2[kE4M3 ? BN * 128 : 16];
+    // e4m3: its third step's buffer, which is free when results leave
+    char *const stage = rows2;
+    constexpr int kHalf = kMx4 ? 8192 : 4096;
+    // 16 bytes for each row, then for each column, twice: mx4's exponents of two steps;
+    // e4m3's row scales of four
+    __shared__ __attribute__((aligned(16))) char scales[kScaled ? 2 * kHalf : 16];   // as planes of dwords
     __shared__ uint32_t first[GRAD ? 1 : XRED_MAX_EXPERTS];   // tile of each expert
-    __shared__ uint32_t shared[4];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t wr = wave / 2, wc = wave % 2;
+    const uint32_t wr = wave / kAcross, wc = wave % kAcross;
     // Work comes in items: a tile, or (p.spans) as many columns' tiles of an expert's last
     // rows as take about as long, two or three if those rows are at most 128 or 64.
     auto span = [&](uint32_t rest) { return p.spans ? rest > 64 ? 2u : 3u : 1u; };
@@ -177,15 +192,15 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
     if constexpr (GRAD) {
         total = share ? p.experts * share * 8 : p.experts * of_expert;
     } else {
-        RowTiles<kProductThreads> all;
-        all.start(p, shared, [&](uint32_t n) {
+        RowTiles<kThreads> all;
+        all.start(p, (uint32_t *)stage, [&](uint32_t n) {
             const uint32_t rest = n % 256, s = span(rest);
             return whole_tiles(n) * p.col_tiles +
                    (rest == 0 || rest > 128 ? 0 : (p.col_tiles + s - 1) / s);
         });
 #pragma unroll
-        for (int j = 0; j < RowTiles<kProductThreads>::kEach; ++j)
-            first[threadIdx.x * RowTiles<kProductThreads>::kEach + j] = all.first[j];
+        for (int j = 0; j < RowTiles<kThreads>::kEach; ++j)
+            first[threadIdx.x * RowTiles<kThreads>::kEach + j] = all.first[j];
         total = __builtin_amdgcn_readfirstlane(all.total);
         __syncthreads();
     }
@@ -201,7 +216,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
     auto next = [&](WideTile &w) {
         if (columns_left) {
             --columns_left;
-            w.column += 256;
+            w.column += BN;
             return true;
         }
         if constexpr (GRAD) {
@@ -217,7 +232,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
             grouped(i, p.row_tiles, p.col_tiles, row, column);
             w.row = row * 256;
             w.rows = p.m - w.row;
-            w.column = column * 256;
+            w.column = column * BN;
             uniform_rows(p, w.expert, lo, hi);
             w.first = lo;
             w.length = hi - lo;
@@ -248,7 +263,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
             }
             w.row = lo + row * 256;
             w.rows = hi - w.row;
-            w.column = column * 256;
+            w.column = column * BN;
             w.length = p.k * P::kSize;
             w.steps = (w.length + 127) / 128;
         }
@@ -259,7 +274,60 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
     Columns columns;
     const lds_bytes r0 = (lds_bytes)rows0, r1 = (lds_bytes)rows1;
     const lds_bytes c0 = (lds_bytes)columns0, c1 = (lds_bytes)columns1;
+    const lds_bytes r2 = (lds_bytes)rows2, c2 = (lds_bytes)columns2;
+    (void)r2, (void)c2;
     const uint32_t column_length = ACROSS ? p.k : 0;
+    // Scales of group g: mx4's exponents of steps 2 g and 2 g + 1, e4m3's row scales of
+    // steps 4 g to 4 g + 3, 16 bytes for each row and column, a thread each.  They go through
+    // registers to their half of `scales`; what lies past a row's end is masked when it is
+    // read, or not read.
+    u32x4 scale_held[2];
+    auto fetch_scales = [&](const WideTile &w, uint32_t g) {
+        if constexpr (kScaled) {
+            const uint32_t tid = fresh_thread(), count = kMx4 ? w.length / 16 : w.steps * 4;
+            auto load = [&](const char *from, uint64_t stride, uint32_t items) {
+                items = items < 256 ? items : 256;
+                const rsrc_t r = make_rsrc(from, (uint32_t)((items - 1) * stride + count));
+                return bload<kLoadKeep>(
+                    r, tid < items ? __umul24(tid, (uint32_t)stride) + g * 16 : kOutside);
+            };
+            scale_held[0] = load(p.row_scale + w.row * p.row_scale_stride, p.row_scale_stride, w.rows);
+            if constexpr (kMx4)
+                scale_held[1] = load(p.col_scale + w.expert * p.col_scale_expert +
+                                         w.column * p.col_scale_stride, p.col_scale_stride, p.n - w.column);
+        }
+    };
+    // A dword of each row and column makes a plane of 256, those of the blocks of 32 that a
+    // lane works on side by side: a lane reads its own at once (several reads would be
+    // merged into one whose place the compiler no longer knows, and which waits for all
+    // loads to LDS).
+    auto put_scales = [&](uint32_t g) {
+        if constexpr (kScaled) {
+            const uint32_t tid = fresh_thread();
+            const lds_bytes to = (lds_bytes)scales + g % 2 * kHalf + tid % 32 * 32 + tid / 32 * 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                *(__attribute__((address_space(3))) uint32_t *)(to + i * 1024) = scale_held[0][i];
+                if constexpr (kMx4)
+                    *(__attribute__((address_space(3))) uint32_t *)(to + 4096 + i * 1024) = scale_held[1][i];
+            }
+        }
+    };
+    // Of `blocks` blocks from block b on, in plane i of group g; base: rows 0, columns 4096.
+    auto scales_at = [&](auto blocks, uint32_t g, uint32_t base, uint32_t i, uint32_t b, uint32_t l,
+                         uint32_t *to) {
+        constexpr int N = decltype(blocks)::value;
+        const lds_bytes from = (lds_bytes)scales + g % 2 * kHalf + base + i * 1024 + l % 32 * 32 + b * 4;
+        if constexpr (N == 4) {
+            const u32x4 v = *(const __attribute__((address_space(3))) u32x4 *)from;
+            to[0] = v[0], to[1] = v[1], to[2] = v[2], to[3] = v[3];
+        } else if constexpr (N == 2) {
+            const u32x2 v = *(const __attribute__((address_space(3))) u32x2 *)from;
+            to[0] = v[0], to[1] = v[1];
+        } else {
+            to[0] = *(const __attribute__((address_space(3))) uint32_t *)from;
+        }
+    };
     // operands of a tile, and its first two steps on their way
     auto begin = [&](const WideTile &w) {
         if (w.steps == 0) return;
@@ -283,6 +351,7 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
             rows.template load<false>(1, w.length, r1);
             columns.template load<false>(1, along, c1);
         }
+        fetch_scales(w, 0);
     };
 
     WideTile w, ahead;
@@ -295,55 +364,153 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
         // the tile by RB blocks of 32 rows a wave
         auto run = [&](auto blocks) {
             constexpr int RB = decltype(blocks)::value;
-            f32x16 acc[RB][4];
+            f32x16 acc[RB][CB];
             const uint32_t l = fresh_thread() % 64, h = l / 32;
-            constexpr int kReads = RB * Rows::kReads + 4 * Columns::kReads, kMma = RB * 4 * (P::kSize == 4 ? 4 : 1);
             const uint32_t whole = GRAD ? w.length / Rows::kRows : w.length / 128;
             const uint32_t along = ACROSS && !GRAD ? column_length : w.length;
-            u32x4 rf[2][RB], cf[2][4];
-            uint32_t re[2][RB], ce[2][4];   // mx4: exponents of a step
-            // where they lie: this lane's rows and columns
-            uint32_t re_at[RB], ce_at[4];
-            const char *re_base = nullptr, *ce_base = nullptr;
-            if constexpr (kMx4) {
-                re_base = p.row_scale + w.row * p.row_scale_stride + 4 * h;
-                ce_base = p.col_scale + w.expert * p.col_scale_expert + w.column * p.col_scale_stride + 4 * h;
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int c = 0; c < CB; ++c) acc[r][c] = f32x16{};
+            if constexpr (kE4M3) {
+            // e4m3: a step is 128 elements of k, which share their scales.  The sums of a
+            // block of rows come from the matrix cores in `part` and join acc, scaled, while
+            // the next block's are on their way.
+            // Half the work a step for as long a way from memory: three steps are in LDS.
+            // Half the work a step for as long a way from memory: three steps are in LDS.
+            u32x4 rf[4], cf[4][CB];
+            f32x16 part[CB];
+            float row_scale[RB], column_scale = 0.0f, last_by = 0.0f;
+            part[CB - 1] = f32x16{};
+            // one for the tile and step, by the scalar cache: a vector load would not end
+            // before the steps that were asked for ahead of it
+            using Scalars = const __attribute__((address_space(4))) float *;
+            const Scalars column_scales =
+                (Scalars)(uintptr_t)(p.col_scale + w.expert * p.col_scale_expert +
+                                     w.column / 128 * p.col_scale_stride);
+            auto scales_of = [&](uint32_t t) {
+                uint32_t v[RB];
+                scales_at(blocks, t / 4, 0, t % 4, wr * RB, l, v);
+#pragma unroll
+                for (int r = 0; r < RB; ++r) row_scale[r] = __uint_as_float(v[r]);
+            };
+            auto read_columns = [&](lds_bytes cs, int half) {
+#pragma unroll
+                for (int s = 2 * half; s < 2 * half + 2; ++s)
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) cf[s][c] = Columns::fragment(cs, wc * CB + c, s, l);
+            };
+            auto read_row = [&](lds_bytes rs, int r, int half) {
+#pragma unroll
+                for (int s = 2 * half; s < 2 * half + 2; ++s) rf[s] = Rows::fragment(rs, wr * RB + r, s, l);
+            };
+            auto join = [&](int r, int c, float by) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[r][c][j] = __builtin_fmaf(part[c][j], by, acc[r][c][j]);
+                // here and not later, when there would be more products waiting to join
+                __asm__ volatile("" : "+v"(acc[r][c]));
+            };
+            // step t in (rt, ct), the next in (rn, cn); FULL: three whole ones follow
+            auto body = [&](auto kind, uint32_t t, lds_bytes rt, lds_bytes ct, lds_bytes rn, lds_bytes cn) {
+                constexpr bool FULL = decltype(kind)::value != 0;
+                const bool go_on = FULL || t + 1 < w.steps;
+                const float next_scale = column_scales[go_on ? t + 1 : t];
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
-                    const uint32_t row = (wr * RB + r) * 32 + l % 32;
-                    re_at[r] = (row < w.rows ? row : w.rows - 1) * (uint32_t)p.row_scale_stride;
+                    const bool last = r + 1 == RB;
+                    if (last) {
+                        if (t % 4 == 2 && t + 2 < w.steps) put_scales(t / 4 + 1);
+                        // the step's fragments have been read, and the next step is there:
+                        // all loads but those of the one after it have ended
+                        if constexpr (FULL) __asm__ volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
+                        else __asm__ volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                        __builtin_amdgcn_s_barrier();
+                        if (t % 4 == 0 && t + 4 < w.steps) fetch_scales(w, t / 4 + 1);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (FULL || t + 3 < w.steps) {
+                            rows.template load<FULL>(t + 3, w.length, rt);
+                            columns.template load<FULL>(t + 3, w.length, ct);
+                        }
+                    }
+                    static_assert(CB == 2, "the order below");
+                    const float by = row_scale[r] * column_scale;
+                    part[0] = multiply_e4m3(cf[0][0], cf[1][0], rf[0], rf[1], f32x16{});
+                    join((r + RB - 1) % RB, 1, last_by);
+                    part[1] = multiply_e4m3(cf[0][1], cf[1][1], rf[0], rf[1], f32x16{});
+                    if (!last) read_row(rt, r + 1, 0);
+                    else if (go_on) read_row(rn, 0, 0), read_columns(cn, 0);
+                    part[0] = multiply_e4m3(cf[2][0], cf[3][0], rf[2], rf[3], part[0]);
+                    part[1] = multiply_e4m3(cf[2][1], cf[3][1], rf[2], rf[3], part[1]);
+                    if (!last) read_row(rt, r + 1, 1);
+                    else if (go_on) read_row(rn, 0, 1), read_columns(cn, 1), scales_of(t + 1);
+                    join(r, 0, by);
+                    last_by = by;
+                    if constexpr (FULL) {
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x20, 4, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x2, 17, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x20, 4, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x20, 4, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x2, 18, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint32_t col = (wc * 4 + c) * 32 + l % 32;
-                    ce_at[c] = (col < p.n - w.column ? col : p.n - w.column - 1) * (uint32_t)p.col_scale_stride;
+                column_scale = next_scale;
+            };
+            using I0 = std::integral_constant<int, 0>;
+            using I1 = std::integral_constant<int, 1>;
+            if (w.steps) {
+                if (w.steps > 2) {
+                    rows.template load<false>(2, w.length, r2);
+                    columns.template load<false>(2, w.length, c2);
                 }
+                column_scale = column_scales[0];
+                read_columns(c0, 0);
+                read_columns(c0, 1);
+                read_row(r0, 0, 0);
+                read_row(r0, 0, 1);
+                scales_of(0);
             }
-            auto exponents = [&](uint32_t t, int to) {
+            uint32_t t = 0;
+            for (; t + 5 < whole; t += 3) {
+                body(I1{}, t, r0, c0, r1, c1);
+                body(I1{}, t + 1, r1, c1, r2, c2);
+                body(I1{}, t + 2, r2, c2, r0, c0);
+            }
+            for (; t < w.steps; t += 3) {
+                body(I0{}, t, r0, c0, r1, c1);
+                if (t + 1 < w.steps) body(I0{}, t + 1, r1, c1, r2, c2);
+                if (t + 2 < w.steps) body(I0{}, t + 2, r2, c2, r0, c0);
+            }
+            join(RB - 1, 1, last_by);
+            } else {
+            constexpr int kReads = RB * Rows::kReads + 4 * Columns::kReads, kMma = RB * 4 * (P::kSize == 4 ? 4 : 1);
+            u32x4 rf[2][RB], cf[2][4];
+            uint32_t re[2][RB], ce[2][4];   // mx4: exponents of a step
+            // of step t, from `scales`; LAST: the row may end in it
+            auto exponents = [&](auto last, uint32_t t, int to) {
                 if constexpr (kMx4) {
-                    const uint32_t count = w.length / 16;   // of a row
-                    auto one = [&](const char *from, uint32_t at) {
-                        if (t * 8 + 8 <= count)
-                            return *(const __attribute__((address_space(1))) u32_any *)((global_bytes)from + t * 8 + at);
-                        uint32_t v = 0;
+                    const bool there = !decltype(last)::value || t * 8 + 4 * h < w.length / 16;
+                    scales_at(blocks, t / 2, 0, t % 2 * 2 + h, wr * RB, l, re[to]);
+                    scales_at(std::integral_constant<int, 4>{}, t / 2, 4096, t % 2 * 2 + h, wc * 4, l, ce[to]);
 #pragma unroll
-                        for (uint32_t j = 0; j < 4; ++j)
-                            if (t * 8 + 4 * h + j < count) v |= (uint32_t)(uint8_t)from[at + t * 8 + j] << (8 * j);
-                        return v;
-                    };
+                    for (int r = 0; r < RB; ++r) re[to][r] = there ? re[to][r] : 0;
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) re[to][r] = one(re_base, re_at[r]);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) ce[to][c] = one(ce_base, ce_at[c]);
+                    for (int c = 0; c < 4; ++c) ce[to][c] = there ? ce[to][c] : 0;
                 }
             };
             auto read = [&](auto sub, lds_bytes rs, lds_bytes cs, int to) {
                 constexpr int S = decltype(sub)::value;
                 // in the order in which they are used
-                cf[to][0] = Columns::fragment(cs, wc * 4, S, l);
+                cf[to][0] = Columns::fragment(cs, wc * CB, S, l);
                 rf[to][0] = Rows::fragment(rs, wr * RB, S, l);
 #pragma unroll
-                for (int c = 1; c < 4; ++c) cf[to][c] = Columns::fragment(cs, wc * 4 + c, S, l);
+                for (int c = 1; c < 4; ++c) cf[to][c] = Columns::fragment(cs, wc * CB + c, S, l);
 #pragma unroll
                 for (int r = 1; r < RB; ++r) rf[to][r] = Rows::fragment(rs, wr * RB + r, S, l);
             };
@@ -369,11 +536,13 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
                             lds_bytes rn, lds_bytes cn) {
                 constexpr bool FULL = decltype(kind)::value != 0, FIRST = decltype(kind)::value == 2;
                 constexpr int E = decltype(parity)::value;
-                constexpr int kScales = kMx4 ? RB + 4 : 0;
-                if (FULL || t + 1 < w.steps) exponents(t + 1, 1 - E);
+                if constexpr (kMx4 && E == 0)
+                    if (FULL || t + 2 < w.steps) fetch_scales(w, t / 2 + 1);
+                if constexpr (kMx4 && E == 1)
+                    if (FULL || t + 1 < w.steps) put_scales(t / 2 + 1);
                 read(I1{}, rt, ct, 1);
                 mma(I0{}, 0, E);
-                if constexpr (FULL) interleave<kReads, kMma, kScales, 0>();
+                if constexpr (FULL) interleave<kReads, kMma, kMx4 && E == 0 ? 2 : 0, kMx4 && E == 1 ? 8 : 0>();
                 __builtin_amdgcn_sched_barrier(0);
                 // the rows of the next step, fetched a step ago, to LDS, and those of the
                 // one after it on their way; the columns follow when their buffer is free,
@@ -399,22 +568,22 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
                 if constexpr (FULL) {
                     columns.template load<true>(t + 2, along, ct);
                     read(I0{}, rn, cn, 0);
+                    exponents(std::false_type{}, t + 1, 1 - E);
                     mma(I3{}, 1, E);
-                    interleave<kReads, kMma, 8, 0>();
+                    interleave<kReads + (kMx4 ? 2 : 0), kMma, 8, 0>();
                     __builtin_amdgcn_sched_barrier(0);
                 } else {
                     if (t + 2 < w.steps) columns.template load<false>(t + 2, along, ct);
-                    if (t + 1 < w.steps) read(I0{}, rn, cn, 0);
+                    if (t + 1 < w.steps) {
+                        read(I0{}, rn, cn, 0);
+                        exponents(std::true_type{}, t + 1, 1 - E);
+                    }
                     mma(I3{}, 1, E);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             };
-#pragma unroll
-            for (int r = 0; r < RB; ++r)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) acc[r][c] = f32x16{};
             if (w.steps) {
-                exponents(0, 0);
+                exponents(std::true_type{}, 0, 0);
                 read(I0{}, r0, c0, 0);
             }
             uint32_t t = 0;
@@ -431,6 +600,8 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
                 if (t + 1 < w.steps) body(I0{}, I1{}, t + 1, r1, c1, r0, c0);
             }
 
+            }
+
             const WideTile done = w;
             w = ahead;
             if (more) begin(w);
@@ -440,43 +611,42 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
             // whole pieces of 16 bytes: a descriptor drops what lies outside
             const bool pieces = !ADD && p.n % (16 / kEs) == 0 && p.out_stride < kWideStride;
             if (pieces) {
-                // Through LDS, 32 rows of 128 bytes at a time, so that stores are of whole
+                // Through LDS, 32 rows of 64 or 128 bytes at a time, so that stores are of whole
                 // lines (32 bytes of a row each, straight from the registers: 6 % slower).
                 // A wave's accesses to LDS happen in order, which is all that its own part
                 // of it needs.
                 const rsrc_t to = make_rsrc(out, kOutside);
                 const lds_bytes mine = (lds_bytes)stage + wave * kStage;
-                constexpr int kWidth = 128 / kEs;
-                behind = RB * 4 * kEs;
+                constexpr int kWidth = kChunk / kEs, kLanes = kChunk / 16;   // of a row
+                behind = RB * CB * kEs;
 #pragma unroll
                 for (int r = 0; r < RB; ++r)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const lds_bytes put = mine + l % 32 * 144 + (kEs == 4 ? h * 16 : c % 2 * 64 + h * 8);
+                    for (int i = 0; i < 4 * CB; ++i) {   // 8 columns each
+                        const int c = i / 4, q = i % 4, part = i % (kWidth / 8);
+                        float v[4];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            float v[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) v[j] = acc[r][c][4 * q + j];
-                            if constexpr (kEs == 4)
-                                *(__attribute__((address_space(3))) u32x4 *)(put + q * 32) =
-                                    u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]),
-                                          __float_as_uint(v[2]), __float_as_uint(v[3])};
-                            else
-                                *(__attribute__((address_space(3))) u32x2 *)(put + q * 16) =
-                                    u32x2{pair_of(v[0], v[1], dtype_of<O>()), pair_of(v[2], v[3], dtype_of<O>())};
-                        }
-                        if (kEs == 2 && c % 2 == 0) continue;
+                        for (int j = 0; j < 4; ++j) v[j] = acc[r][c][4 * q + j];
+                        const lds_bytes put = mine + l % 32 * kPitch + (part * 8 + h * 4) * kEs;
+                        if constexpr (kEs == 4)
+                            *(__attribute__((address_space(3))) u32x4 *)put =
+                                u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]),
+                                      __float_as_uint(v[2]), __float_as_uint(v[3])};
+                        else
+                            *(__attribute__((address_space(3))) u32x2 *)put =
+                                u32x2{pair_of(v[0], v[1], dtype_of<O>()), pair_of(v[2], v[3], dtype_of<O>())};
+                        if (part != kWidth / 8 - 1) continue;
                         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t row = j * 8 + l / 8, in_tile = (wr * RB + r) * 32 + row;
-                            const uint32_t col = done.column + (wc * 4 + (kEs == 4 ? c : c - 1)) * 32 +
-                                                 l % 8 * (kWidth / 8);
-                            const u32x4 v = *(const __attribute__((address_space(3))) u32x4 *)(
-                                mine + row * 144 + l % 8 * 16);
+                        for (int j = 0; j < kLanes / 2; ++j) {
+                            const uint32_t row = j * (64 / kLanes) + l / kLanes;
+                            const uint32_t in_tile = (wr * RB + r) * 32 + row;
+                            const uint32_t col = done.column + wc * (32 * CB) + (i + 1) * 8 - kWidth +
+                                                 l % kLanes * (16 / kEs);
+                            const u32x4 x = *(const __attribute__((address_space(3))) u32x4 *)(
+                                mine + row * kPitch + l % kLanes * 16);
                             const bool in = in_tile < done.rows && col < p.n;
-                            bstore<kStoreKeep>(v, to, in ? in_tile * (uint32_t)p.out_stride + col * kEs : kOutside);
+                            bstore<kStoreKeep>(x, to, in ? in_tile * (uint32_t)p.out_stride + col * kEs : kOutside);
                         }
                         __builtin_amdgcn_wave_barrier();
                     }
@@ -487,10 +657,10 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
                     const uint32_t row = (wr * RB + r) * 32 + l % 32;
                     char *to = out + row * p.out_stride;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < CB; ++c)
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const uint32_t col = done.column + (wc * 4 + c) * 32 + 8 * q + 4 * h;
+                            const uint32_t col = done.column + (wc * CB + c) * 32 + 8 * q + 4 * h;
                             if (row >= done.rows || col >= p.n) continue;
                             const uint32_t n = p.n - col < 4 ? p.n - col : 4;
                             float v[4];
@@ -511,7 +681,9 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
         else if (behind == 32) __asm__ volatile("s_waitcnt vmcnt(32)" ::: "memory");
         else if (behind == 16) __asm__ volatile("s_waitcnt vmcnt(16)" ::: "memory");
         else if (behind == 8) __asm__ volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        else if (behind == 4) __asm__ volatile("s_waitcnt vmcnt(4)" ::: "memory");
         else __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (w.steps) put_scales(0);
         __syncthreads();
         // at most a half or a quarter of the rows: the waves share them differently
         if (w.rows > 128) run(std::integral_constant<int, 4>{});
@@ -521,9 +693,25 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
 }
 
 template <class P, class O, bool GRAD, bool ACROSS, bool ADD>
+__global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(ProductParams p)
+{
+    product_wide<P, O, GRAD, ACROSS, ADD>(p);
+}
+
+// With at most 256 registers the compiler lets matrix instructions write to those that
+// vector instructions read; with more, to the others, each value moved before it is used.
+template <class P, class O>
+__global__ __launch_bounds__(kProductThreads, 1) __attribute__((amdgpu_num_vgpr(256))) void
+product_wide_e4m3_kernel(ProductParams p)
+{
+    product_wide<P, O, false, false, false>(p);
+}
+
+template <class P, class O, bool GRAD, bool ACROSS, bool ADD>
 hipError_t go_wide(ProductParams p, hipStream_t s)
 {
-    p.col_tiles = (p.n + 255) / 256;
+    constexpr uint32_t BN = wide_columns<P>();
+    p.col_tiles = (p.n + BN - 1) / BN;
     p.row_tiles = (p.m + 255) / 256;
     const uint64_t tiles = (GRAD ? (uint64_t)p.experts * p.row_tiles
                                  : p.rows / 256 + (p.rows < p.experts ? p.rows : p.experts)) * p.col_tiles;
@@ -532,7 +720,10 @@ hipError_t go_wide(ProductParams p, hipStream_t s)
     // even out what workgroups do where each has enough items (12 a CU: 678 us without, 653
     // with; 6 a CU: 755 and 892, an item more or less being a fifth of the time)
     p.spans = tiles >= 8 * cus;
-    return launch_kernel(product_wide_kernel<P, O, GRAD, ACROSS, ADD>,
+    void (*kernel)(ProductParams);
+    if constexpr (__is_same(P, PE4M3)) kernel = product_wide_e4m3_kernel<P, O>;
+    else kernel = product_wide_kernel<P, O, GRAD, ACROSS, ADD>;
+    return launch_kernel(kernel,
                          dim3(grid_of(tiles < cus ? (tiles + 7) / 8 * 8 : cus, kProductThreads)),
                          dim3(kProductThreads), 0, s, p);
 }
