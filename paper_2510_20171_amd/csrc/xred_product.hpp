@@ -102,98 +102,25 @@ __device__ __forceinline__ f32x16 multiply_mx4(u32x4 c, u32x4 r, uint32_t cs, ui
 __device__ const u32x4 product_zeros = {0, 0, 0, 0};
 
 // ---------------------------------------------------------------- operands --
-// One operand's pieces of a tile of N rows (along) or columns (across): kPieces a
-// thread and step, on their way into LDS or into registers.
-template <class P, bool ACROSS, bool DIRECT, int N>
-struct Operand {
+// The operand of a tile's N rows (along) or columns (across), in pieces of 16 bytes,
+// kPieces a thread and step.
+template <class P, bool ACROSS, int N>
+struct Pieces {
     static constexpr int kPieces = N * 128 / 16 / kProductThreads;
     static constexpr int kWide = N * P::kSize / 16;   // across: pieces of a row of k
     static constexpr int kRows = 128 / P::kSize;      // across: rows of k in a step
-    static constexpr int kPer = 16 / P::kSize;        // elements of a piece
 
-    const char *base;
-    uint64_t step;            // bytes from one step to the next
-    uint64_t at[kPieces];     // from base: this thread's pieces
-    uint32_t k[kPieces];      // along: byte of k within a step; across: row of k
-    int32_t have[kPieces];    // across: bytes of the piece that exist, below 0 none
-    u32x4 held[DIRECT ? 1 : kPieces];
-
-    static __device__ __forceinline__ uint32_t slot(int i)
+    // Place i in LDS of thread tid, in pieces; what lies there: a row, and a piece of it.
+    static __device__ __forceinline__ uint32_t slot(int i, uint32_t tid)
     {
-        return ((threadIdx.x / 64) * kPieces + i) * 64 + threadIdx.x % 64;
+        return (tid / 64 * kPieces + i) * 64 + tid % 64;
     }
-
-    // items: rows (along) or columns (across) that exist, at least one; those
-    // behind them are read as others, whose products nobody stores.
-    __device__ __forceinline__ void start(const char *from, uint64_t stride, uint32_t items)
+    static __device__ __forceinline__ uint32_t row_of(uint32_t q) { return ACROSS ? q / kWide : q / 8; }
+    static __device__ __forceinline__ uint32_t piece_of(uint32_t q)
     {
-        base = from;
-        step = ACROSS ? stride * kRows : 128;
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const uint32_t q = slot(i);
-            if constexpr (ACROSS) {
-                const uint32_t row = q / kWide;
-                uint32_t piece = q % kWide;
-                if constexpr (P::kSize == 2) piece ^= (row % 4) * 2;
-                const int32_t left = (int32_t)(items * P::kSize) - (int32_t)piece * 16;
-                k[i] = row;
-                have[i] = left;
-                at[i] = row * stride + (left > 0 ? piece * 16 : 0);
-            } else {
-                const uint32_t row = q / 8, piece = q % 8 ^ row % 8;
-                k[i] = piece * 16;
-                at[i] = (row < items ? row : items - 1) * stride + piece * 16;
-            }
-        }
-    }
-
-    // Step t of k into `to` (DIRECT) or into registers.  length: of k, in bytes
-    // (along) or rows (across).
-    __device__ __forceinline__ void load(uint32_t t, uint32_t length, lds_bytes to)
-    {
-        const uint32_t done = t * (ACROSS ? kRows : 128), left = length - done;
-        const bool whole = left >= (ACROSS ? kRows : 128);
-        const char *from = base + t * step;
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            if constexpr (DIRECT) {
-                const char *src = from + at[i];
-                if (!whole && k[i] >= left) src = (const char *)&product_zeros;
-                __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void *)src,
-                    (__attribute__((address_space(3))) void *)(to + ((threadIdx.x / 64) * kPieces + i) * 1024),
-                    16, 0, 0);
-            } else {
-                const char *src = from + at[i];
-                int32_t bytes = ACROSS ? (k[i] < left ? have[i] : 0) : (int32_t)left - (int32_t)k[i];
-                if (bytes >= 16) {
-                    held[i] = *(const __attribute__((address_space(1))) u32x4_any *)(global_bytes)src;
-                } else {
-                    u32x4 v = {0, 0, 0, 0};
-#pragma unroll
-                    for (int j = 0; j < kPer; ++j)
-                        if (j * P::kSize < bytes) {
-                            if constexpr (P::kSize == 4)
-                                v[j] = *(const uint32_t *)(src + j * 4);
-                            else if constexpr (P::kSize == 2)
-                                v[j / 2] |= (uint32_t)*(const uint16_t *)(src + j * 2) << (16 * (j % 2));
-                            else
-                                v[j / 4] |= (uint32_t)*(const uint8_t *)(src + j) << (8 * (j % 4));
-                        }
-                    held[i] = v;
-                }
-            }
-        }
-    }
-
-    // What load() left in registers, to LDS.
-    __device__ __forceinline__ void store(lds_bytes to) const
-    {
-        if constexpr (!DIRECT)
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                *(__attribute__((address_space(3))) u32x4 *)(to + slot(i) * 16) = held[i];
+        if constexpr (!ACROSS) return q % 8 ^ q / 8 % 8;
+        const uint32_t piece = q % kWide;
+        return P::kSize == 2 ? piece ^ q / kWide % 4 * 2 : piece;
     }
 
     // Sub-step s of block b of 32.
@@ -223,6 +150,162 @@ struct Operand {
                 v[j] = *(const __attribute__((address_space(3))) uint32_t *)(p + j * (N * 4));
             return v;
         }
+    }
+};
+
+// An operand whose pieces lie on the 16-byte grid, whole ones only: straight to LDS.
+template <class P, bool ACROSS, int N>
+struct GridOperand : Pieces<P, ACROSS, N> {
+    using Base = Pieces<P, ACROSS, N>;
+    static constexpr int kPieces = Base::kPieces, kRows = Base::kRows;
+    const char *base;
+    uint64_t step;            // bytes from one step to the next
+    uint64_t at[kPieces];     // from base: this thread's pieces
+
+    // items: rows (along) or columns (across) that exist, at least one; those
+    // behind them are read as others, whose products nobody stores.
+    __device__ __forceinline__ void start(const char *from, uint64_t stride, uint32_t items, uint32_t)
+    {
+        base = from;
+        step = ACROSS ? stride * kRows : 128;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t q = Base::slot(i, threadIdx.x), row = Base::row_of(q), at16 = Base::piece_of(q) * 16;
+            if constexpr (ACROSS) at[i] = row * stride + (at16 < items * P::kSize ? at16 : 0);
+            else at[i] = (row < items ? row : items - 1) * stride + at16;
+        }
+    }
+
+    // Step t of k to `to`.  length: of k, in bytes (along) or rows (across).
+    __device__ __forceinline__ void load(uint32_t t, uint32_t length, lds_bytes to)
+    {
+        const uint32_t left = length - t * (ACROSS ? kRows : 128);
+        const bool whole = left >= (ACROSS ? kRows : 128);
+        const char *from = base + t * step;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const char *src = from + at[i];
+            const uint32_t q = Base::slot(i, threadIdx.x);
+            if (!whole && (ACROSS ? Base::row_of(q) : Base::piece_of(q) * 16) >= left)
+                src = (const char *)&product_zeros;
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void *)src,
+                (__attribute__((address_space(3))) void *)(to + (threadIdx.x / 64 * kPieces + i) * 1024),
+                16, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void store(uint32_t, uint32_t, lds_bytes) const {}
+};
+
+// Bytes [skip, skip + n) of v, zeros behind them.
+__device__ __forceinline__ u32x4 bytes_of(u32x4 v, uint32_t skip, uint32_t n)
+{
+    uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+    if (skip >= 8) lo = hi, hi = 0, skip -= 8;
+    if (skip >= 8) lo = 0;
+    else if (skip) lo = lo >> 8 * skip | hi << (64 - 8 * skip), hi >>= 8 * skip;
+    if (n < 8) lo &= ((uint64_t)1 << 8 * n) - 1, hi = 0;
+    else if (n < 16) hi &= ((uint64_t)1 << 8 * (n - 8)) - 1;
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
+// An operand at any element, of any length: by way of registers.  A piece is read whole,
+// with what follows it in memory; only in the operand's last steps does that matter, where
+// a piece past the end is read as its last 16 bytes, shifted into place, and what is past
+// the end of k becomes zero.  Offset: of an offset within a step.
+template <class P, bool ACROSS, int N, class Offset>
+struct LooseOperand : Pieces<P, ACROSS, N> {
+    using Base = Pieces<P, ACROSS, N>;
+    static constexpr int kPieces = Base::kPieces, kRows = Base::kRows;
+    const char *base;
+    uint64_t step, bytes;   // from one step to the next; from base to the operand's end
+    Offset at[kPieces];
+    u32x4 held[kPieces];
+
+    // length: of k, in bytes (along) or rows (across), at least one.
+    __device__ __forceinline__ void start(const char *from, uint64_t stride, uint32_t items,
+                                          uint32_t length, uint32_t tid = threadIdx.x)
+    {
+        base = from;
+        step = ACROSS ? stride * kRows : 128;
+        bytes = ACROSS ? (length - 1) * stride + (uint64_t)items * P::kSize
+                       : (uint64_t)(items - 1) * stride + length;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t q = Base::slot(i, tid), row = Base::row_of(q), at16 = Base::piece_of(q) * 16;
+            if constexpr (ACROSS) at[i] = row * (Offset)stride + (at16 < items * P::kSize ? at16 : 0);
+            else at[i] = (row < items ? row : items - 1) * (Offset)stride + at16;
+        }
+    }
+
+    // Where piece i of step t begins; false: past the end of k.  left: bytes of it before that
+    __device__ __forceinline__ bool place(int i, uint32_t t, uint32_t length, uint64_t &off, uint32_t &left) const
+    {
+        const uint32_t q = Base::slot(i, threadIdx.x);
+        const uint32_t k = t * (ACROSS ? kRows : 128) + (ACROSS ? Base::row_of(q) : Base::piece_of(q) * 16);
+        left = ACROSS ? 16 : length - k;
+        off = t * step + at[i];
+        return k < length;
+    }
+
+    // WHOLE: step t ends before the last row of k (across) or a row's end (along).
+    template <bool WHOLE>
+    __device__ __forceinline__ void fetch(uint32_t t, uint32_t length)
+    {
+        using Vec = const __attribute__((address_space(1))) u32x4_any;
+        if constexpr (WHOLE) {
+            const char *from = base + t * step;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) held[i] = *(Vec *)((global_bytes)from + at[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                uint64_t off;
+                uint32_t left;
+                if (!place(i, t, length, off, left)) {
+                    held[i] = u32x4{0, 0, 0, 0};
+                } else if (bytes >= 16) {
+                    held[i] = *(Vec *)((global_bytes)base + (off < bytes - 16 ? off : bytes - 16));
+                } else {   // an operand of a few elements, one by one
+                    u32x4 v = {0, 0, 0, 0};
+                    for (uint32_t j = 0; j < 16 && off + j < bytes; ++j)
+                        v[j / 4] |= (uint32_t)(uint8_t)base[off + j] << 8 * (j % 4);
+                    held[i] = v;
+                }
+            }
+        }
+    }
+    template <bool WHOLE>
+    __device__ __forceinline__ void put(uint32_t t, uint32_t length, lds_bytes to) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            u32x4 v = held[i];
+            if constexpr (!WHOLE) {
+                uint64_t off;
+                uint32_t left;
+                if (place(i, t, length, off, left)) {
+                    const uint64_t skip = bytes >= 16 && off > bytes - 16 ? off - (bytes - 16) : 0;
+                    v = bytes_of(v, skip < 16 ? (uint32_t)skip : 16, left < 16 ? left : 16);
+                }
+            }
+            *(__attribute__((address_space(3))) u32x4 *)(to + Base::slot(i, threadIdx.x) * 16) = v;
+        }
+    }
+    // Whether step t is whole, and rows of at least 16 bytes follow.
+    __device__ __forceinline__ bool whole(uint32_t t, uint32_t length) const
+    {
+        return ACROSS ? (t + 2) * kRows <= length : (t + 1) * 128 <= length;
+    }
+    __device__ __forceinline__ void load(uint32_t t, uint32_t length, lds_bytes)
+    {
+        if (whole(t, length)) fetch<true>(t, length);
+        else fetch<false>(t, length);
+    }
+    __device__ __forceinline__ void store(uint32_t t, uint32_t length, lds_bytes to) const
+    {
+        if (whole(t, length)) put<true>(t, length, to);
+        else put<false>(t, length, to);
     }
 };
 
@@ -342,8 +425,8 @@ template <class P, bool GRAD, bool ACROSS, bool DIRECT, int RB, int CB>
 __global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams p)
 {
     constexpr int BM = 64 * RB, BN = 64 * CB;
-    using Rows = Operand<P, GRAD, DIRECT, BM>;
-    using Columns = Operand<P, ACROSS, DIRECT, BN>;
+    using Rows = std::conditional_t<DIRECT, GridOperand<P, GRAD, BM>, LooseOperand<P, GRAD, BM, uint64_t>>;
+    using Columns = std::conditional_t<DIRECT, GridOperand<P, ACROSS, BN>, LooseOperand<P, ACROSS, BN, uint64_t>>;
     // two steps, each an array of its own: a read of one does not wait for loads into
     // the other
     __shared__ __attribute__((aligned(1024))) char rows0[BM * 128], rows1[BM * 128];
@@ -391,8 +474,10 @@ __global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams 
         }
         Rows rows;
         Columns columns;
-        rows.start(from, p.row_stride, items);
-        columns.start(col_from, p.col_stride, p.n - n0);
+        // across operands count k in rows
+        const uint32_t col_length = ACROSS && !GRAD ? p.k : length;
+        rows.start(from, p.row_stride, items, length);
+        columns.start(col_from, p.col_stride, p.n - n0, col_length);
         f32x16 acc[RB][CB];
 #pragma unroll
         for (int r = 0; r < RB; ++r)
@@ -401,8 +486,6 @@ __global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams 
 
         const uint32_t per = GRAD ? Rows::kRows : 128;
         const uint32_t steps = (length + per - 1) / per;
-        // across operands count k in rows
-        const uint32_t col_length = ACROSS && !GRAD ? p.k : length;
         // where this lane's rows and columns have their scales
         const char *rs[RB], *cs[CB];
         if constexpr (__is_same(P, PE4M3) || __is_same(P, PMx4)) {
@@ -494,8 +577,8 @@ __global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams 
             }
             multiply_step(t, rt, ct);
             if (t + 1 < steps) {
-                rows.store(rn);
-                columns.store(cn);
+                rows.store(t + 1, length, rn);
+                columns.store(t + 1, col_length, cn);
             }
             __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
@@ -503,8 +586,8 @@ __global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams 
         if (steps) {
             rows.load(0, length, r0);
             columns.load(0, col_length, c0);
-            rows.store(r0);
-            columns.store(c0);
+            rows.store(0, length, r0);
+            columns.store(0, col_length, c0);
             __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             for (uint32_t t = 0; t < steps; t += 2) {

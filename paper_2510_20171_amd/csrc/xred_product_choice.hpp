@@ -14,6 +14,16 @@ inline bool wide_pays(const ProductParams &p, bool grad)
     return p.n > 128 && rows * columns >= 128;
 }
 
+// Tiles of 64 x 64 where there are too few of 128 x 128 to keep the chip busy.
+template <class P, bool GRAD, bool ACROSS, bool DIRECT>
+hipError_t go_tiles(const ProductParams &p, hipStream_t s)
+{
+    const uint64_t rows = GRAD ? (uint64_t)p.experts * ((p.m + 127) / 128)
+                               : p.rows / 128 + (p.rows < p.experts ? p.rows : p.experts);
+    return rows * ((p.n + 127) / 128) < 2 * device_cus() ? go_product<P, GRAD, ACROSS, DIRECT, 1, 1>(p, s)
+                                                        : go_product<P, GRAD, ACROSS, DIRECT, 2, 2>(p, s);
+}
+
 template <class P>
 hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, hipStream_t s)
 {
@@ -28,13 +38,10 @@ hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, 
                    : launch_wide<P, typename OwnType<P>::T>(p, grad, across, s);
     }
     if (grad)
-        return direct ? go_product<P, true, true, true, 2, 2>(p, s)
-                      : go_product<P, true, true, false, 2, 2>(p, s);
+        return direct ? go_tiles<P, true, true, true>(p, s) : go_tiles<P, true, true, false>(p, s);
     if (across)
-        return direct ? go_product<P, false, true, true, 2, 2>(p, s)
-                      : go_product<P, false, true, false, 2, 2>(p, s);
-    return direct ? go_product<P, false, false, true, 2, 2>(p, s)
-                  : go_product<P, false, false, false, 2, 2>(p, s);
+        return direct ? go_tiles<P, false, true, true>(p, s) : go_tiles<P, false, true, false>(p, s);
+    return direct ? go_tiles<P, false, false, true>(p, s) : go_tiles<P, false, false, false>(p, s);
 }
 
 // Whether scales can be read by whole words (mx4: its exponents, four of them).
@@ -57,8 +64,7 @@ hipError_t launch_product_scaled(const ProductParams &p, hipStream_t s)
         return p.out_type == XRED_FLOAT32    ? launch_wide<P, TF32>(p, false, false, s)
                : p.out_type == XRED_BFLOAT16 ? launch_wide<P, TBF16>(p, false, false, s)
                                              : launch_wide<P, TF16>(p, false, false, s);
-    return direct ? go_product<P, false, false, true, 2, 2>(p, s)
-                  : go_product<P, false, false, false, 2, 2>(p, s);
+    return direct ? go_tiles<P, false, false, true>(p, s) : go_tiles<P, false, false, false>(p, s);
 }
 
 }  // namespace xred

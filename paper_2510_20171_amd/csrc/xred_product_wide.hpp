@@ -123,7 +123,7 @@ struct WideOperand {
 
     static __device__ __forceinline__ u32x4 fragment(lds_bytes from, int b, int s, uint32_t lane)
     {
-        return Operand<P, ACROSS, true, N>::fragment(from, b, s, lane);
+        return Pieces<P, ACROSS, N>::fragment(from, b, s, lane);
     }
 };
 
