@@ -109,6 +109,7 @@ struct Pieces {
     static constexpr int kPieces = N * 128 / 16 / kProductThreads;
     static constexpr int kWide = N * P::kSize / 16;   // across: pieces of a row of k
     static constexpr int kRows = 128 / P::kSize;      // across: rows of k in a step
+    static constexpr int kReads = ACROSS ? (P::kSize == 2 ? 2 : 4) : 1;   // of LDS for a fragment
 
     // Place i in LDS of thread tid, in pieces; what lies there: a row, and a piece of it.
     static __device__ __forceinline__ uint32_t slot(int i, uint32_t tid)
@@ -266,11 +267,14 @@ struct LooseOperand : Pieces<P, ACROSS, N> {
                     held[i] = u32x4{0, 0, 0, 0};
                 } else if (bytes >= 16) {
                     held[i] = *(Vec *)((global_bytes)base + (off < bytes - 16 ? off : bytes - 16));
-                } else {   // an operand of a few elements, one by one
-                    u32x4 v = {0, 0, 0, 0};
-                    for (uint32_t j = 0; j < 16 && off + j < bytes; ++j)
-                        v[j / 4] |= (uint32_t)(uint8_t)base[off + j] << 8 * (j % 4);
-                    held[i] = v;
+                } else {   // an operand of a few elements, byte by byte
+                    uint64_t lo = 0, hi = 0;
+#pragma clang loop unroll(disable)
+                    for (uint64_t j = off < bytes ? bytes - off : 0; j-- > 0;) {
+                        hi = hi << 8 | lo >> 56;
+                        lo = lo << 8 | (uint8_t)base[off + j];
+                    }
+                    held[i] = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
                 }
             }
         }
@@ -278,33 +282,48 @@ struct LooseOperand : Pieces<P, ACROSS, N> {
     template <bool WHOLE>
     __device__ __forceinline__ void put(uint32_t t, uint32_t length, lds_bytes to) const
     {
+        put<WHOLE>(t, length, to, held);
+    }
+    // The same of pieces kept elsewhere.  An operand of at least 16 bytes, whatever the step:
+    // no branch, so that the compiler can count what is on its way.
+    __device__ __forceinline__ void fetch_any(uint32_t t, u32x4 (&v)[kPieces]) const
+    {
+        const uint64_t from = t * step, most = bytes - 16;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            u32x4 v = held[i];
+            const uint64_t off = from + at[i];
+            v[i] = *(const __attribute__((address_space(1))) u32x4_any *)((global_bytes)base + (off < most ? off : most));
+        }
+    }
+    template <bool WHOLE>
+    __device__ __forceinline__ void put(uint32_t t, uint32_t length, lds_bytes to, const u32x4 (&pieces)[kPieces]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            u32x4 v = pieces[i];
             if constexpr (!WHOLE) {
                 uint64_t off;
                 uint32_t left;
-                if (place(i, t, length, off, left)) {
-                    const uint64_t skip = bytes >= 16 && off > bytes - 16 ? off - (bytes - 16) : 0;
-                    v = bytes_of(v, skip < 16 ? (uint32_t)skip : 16, left < 16 ? left : 16);
-                }
+                const bool there = place(i, t, length, off, left);
+                const uint64_t skip = bytes >= 16 && off > bytes - 16 ? off - (bytes - 16) : 0;
+                v = bytes_of(v, skip < 16 ? (uint32_t)skip : 16, !there ? 0 : left < 16 ? left : 16);
             }
             *(__attribute__((address_space(3))) u32x4 *)(to + Base::slot(i, threadIdx.x) * 16) = v;
         }
     }
     // Whether step t is whole, and rows of at least 16 bytes follow.
-    __device__ __forceinline__ bool whole(uint32_t t, uint32_t length) const
+    static __device__ __forceinline__ bool is_whole(uint32_t t, uint32_t length)
     {
         return ACROSS ? (t + 2) * kRows <= length : (t + 1) * 128 <= length;
     }
     __device__ __forceinline__ void load(uint32_t t, uint32_t length, lds_bytes)
     {
-        if (whole(t, length)) fetch<true>(t, length);
+        if (is_whole(t, length)) fetch<true>(t, length);
         else fetch<false>(t, length);
     }
     __device__ __forceinline__ void store(uint32_t t, uint32_t length, lds_bytes to) const
     {
-        if (whole(t, length)) put<true>(t, length, to);
+        if (is_whole(t, length)) put<true>(t, length, to);
         else put<false>(t, length, to);
     }
 };
@@ -421,8 +440,10 @@ __device__ __forceinline__ float value_at(const char *row, uint32_t c, xred_dtyp
 
 // ------------------------------------------------------------------ kernel --
 // 4 waves, two by two, each RB x CB blocks of 32 x 32: tiles of 64 RB x 64 CB.
+// Two of the larger tiles or four of the smaller have to fit a CU: while one waits for its
+// loads, another multiplies (one: 4200 us where two take 2210).
 template <class P, bool GRAD, bool ACROSS, bool DIRECT, int RB, int CB>
-__global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams p)
+__global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kernel(ProductParams p)
 {
     constexpr int BM = 64 * RB, BN = 64 * CB;
     using Rows = std::conditional_t<DIRECT, GridOperand<P, GRAD, BM>, LooseOperand<P, GRAD, BM, uint64_t>>;
@@ -437,20 +458,24 @@ __global__ __launch_bounds__(kProductThreads) void product_kernel(ProductParams 
     const uint32_t wr = wave / 2, wc = wave % 2;   // this wave's place
     RowTiles<kProductThreads> all;
     uint32_t total;
+    // gradient: an expert's tiles are dealt to all XCDs where there are enough of them,
+    // since experts' rows, and with them the tiles' lengths, differ
+    const uint32_t of_expert = p.row_tiles * p.col_tiles, share = of_expert < 64 ? 0 : (of_expert + 7) / 8;
     if constexpr (GRAD) {
-        total = p.experts * p.row_tiles * p.col_tiles;
+        total = share ? p.experts * share * 8 : p.experts * of_expert;
     } else {
         all.start(p, shared, [](uint32_t n) { return (n + BM - 1) / BM; });
         total = all.total * p.col_tiles;
     }
     for (uint32_t i = blockIdx.x; i / 8 < (total + 7) / 8; i += gridDim.x) {
-        uint32_t tile;
-        if (!tile_of(i, total, tile)) continue;
+        uint32_t tile = i;
+        if (!(GRAD && share) && !tile_of(i, total, tile)) continue;
         uint32_t e, m0, n0, items, length;   // expert; first row, column; rows; of k
         const char *from, *col_from;
         if constexpr (GRAD) {
-            e = tile / (p.row_tiles * p.col_tiles);
-            const uint32_t rest = tile - e * p.row_tiles * p.col_tiles;
+            e = share ? tile / 8 / share : tile / of_expert;
+            const uint32_t rest = share ? tile % 8 * share + tile / 8 % share : tile % of_expert;
+            if (rest >= of_expert) continue;
             m0 = rest % p.row_tiles * BM;
             n0 = rest / p.row_tiles * BN;
             uint32_t lo, hi;

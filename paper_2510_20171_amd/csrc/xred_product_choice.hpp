@@ -1,7 +1,7 @@
 // xred_product_choice.hpp -- which kernel takes a product, by types, sizes and alignment.
 #pragma once
 
-#include "xred_product_wide.hpp"
+#include "xred_product_narrow.hpp"
 
 namespace xred {
 
@@ -12,6 +12,13 @@ inline bool wide_pays(const ProductParams &p, bool grad)
     const uint64_t rows = grad ? (uint64_t)p.experts * ((p.m + 255) / 256)
                                : p.rows / 256 + (p.rows < p.experts ? p.rows : p.experts);
     return p.n > 128 && rows * columns >= 128;
+}
+
+// Few rows for an expert: its weights are what costs.  (At 64 elements and more, which
+// pieces and mx4's exponents are read in whole.)
+inline bool narrow_pays(const ProductParams &p)
+{
+    return p.rows <= 16ull * p.experts && p.n >= 64 && p.k >= 64 && p.row_stride < kWideStride && p.col_stride < kWideStride;
 }
 
 // Tiles of 64 x 64 where there are too few of 128 x 128 to keep the chip busy.
@@ -32,10 +39,21 @@ hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, 
                                    on_grid(p.col, p.col_stride, 0, p.n * es)
                              : on_grid(p.row, p.row_stride, 0, p.k * es) &&
                                    on_grid(p.col, p.col_stride, p.col_expert, (across ? p.n : p.k) * es);
-    if (direct && p.row_stride < kWideStride && p.col_stride < kWideStride && wide_pays(p, grad)) {
-        return p.out_type == XRED_FLOAT32
-                   ? launch_wide<P, TF32>(p, grad, across, s)
-                   : launch_wide<P, typename OwnType<P>::T>(p, grad, across, s);
+    if (!grad && narrow_pays(p)) {
+        if (across)
+            return direct ? go_narrow<P, true, true>(p, s) : go_narrow<P, true, false>(p, s);
+        return direct ? go_narrow<P, false, true>(p, s) : go_narrow<P, false, false>(p, s);
+    }
+    if (p.row_stride < kWideStride && p.col_stride < kWideStride && wide_pays(p, grad)) {
+        using O = typename OwnType<P>::T;
+        if (direct)
+            return p.out_type == XRED_FLOAT32 ? launch_wide<P, TF32>(p, grad, across, s)
+                                              : launch_wide<P, O>(p, grad, across, s);
+        // 32768 rows, 64 experts, 4097 x 2049 bf16: 1390 us, tiles of 128 x 128 2160;
+        // transposed 1050 and 2090
+        if (!grad && p.out_type == dtype_of<O>())
+            return across ? go_wide<P, O, false, true, false, false>(p, s)
+                          : go_wide<P, O, false, false, false, false>(p, s);
     }
     if (grad)
         return direct ? go_tiles<P, true, true, true>(p, s) : go_tiles<P, true, true, false>(p, s);
@@ -59,6 +77,8 @@ hipError_t launch_product_scaled(const ProductParams &p, hipStream_t s)
 {
     const bool direct = on_grid(p.row, p.row_stride, 0, p.k) &&
                         on_grid(p.col, p.col_stride, p.col_expert, p.k);
+    if (narrow_pays(p))
+        return direct ? go_narrow<P, false, true>(p, s) : go_narrow<P, false, false>(p, s);
     if (direct && p.row_stride < kWideStride && p.col_stride < kWideStride && scale_words<P>(p) &&
         wide_pays(p, false))
         return p.out_type == XRED_FLOAT32    ? launch_wide<P, TF32>(p, false, false, s)

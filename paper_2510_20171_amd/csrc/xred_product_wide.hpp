@@ -43,11 +43,9 @@ __device__ __forceinline__ void interleave()
 
 // N rows (along) or columns (across) of an operand, a tile's.
 template <class P, bool ACROSS, int N>
-struct WideOperand {
-    static constexpr int kPieces = N / 32;             // of a thread and step
-    static constexpr int kWide = N * P::kSize / 16;    // across: pieces of a row of k
-    static constexpr int kRows = 128 / P::kSize;       // across: rows of k in a step
-    static constexpr int kReads = ACROSS ? (P::kSize == 2 ? 2 : 4) : 1;   // of a fragment
+struct WideOperand : Pieces<P, ACROSS, N> {
+    using Base = Pieces<P, ACROSS, N>;
+    static constexpr int kPieces = Base::kPieces, kRows = Base::kRows;
 
     const char *base;      // the same in every lane
     uint64_t step, bytes;  // from one step to the next; from base to the operand's end
@@ -64,16 +62,9 @@ struct WideOperand {
                        : (uint64_t)(items < N ? items - 1 : N - 1) * stride + length;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const uint32_t q = (tid / 64 * kPieces + i) * 64 + tid % 64;
-            if constexpr (ACROSS) {
-                const uint32_t row = q / kWide;
-                uint32_t piece = q % kWide;
-                if constexpr (P::kSize == 2) piece ^= (row % 4) * 2;
-                at[i] = piece * 16 < items * P::kSize ? row * (uint32_t)stride + piece * 16 : kOutside;
-            } else {
-                const uint32_t row = q / 8, piece = q % 8 ^ row % 8;
-                at[i] = row < items ? row * (uint32_t)stride + piece * 16 : kOutside;
-            }
+            const uint32_t q = Base::slot(i, tid), row = Base::row_of(q), piece = Base::piece_of(q);
+            const bool there = ACROSS ? piece * 16 < items * P::kSize : row < items;
+            at[i] = there ? row * (uint32_t)stride + piece * 16 : kOutside;
         }
     }
 
@@ -88,8 +79,7 @@ struct WideOperand {
     {
         if constexpr (ACROSS || WHOLE) return at[i];
         // the end of a row is not the end of the operand
-        const uint32_t q = (threadIdx.x / 64 * kPieces + i) * 64 + threadIdx.x % 64;
-        return (q % 8 ^ q / 8 % 8) * 16 < length - t * 128 ? at[i] : kOutside;
+        return Base::piece_of(Base::slot(i, threadIdx.x)) * 16 < length - t * 128 ? at[i] : kOutside;
     }
 
     // Step t straight into LDS.
@@ -105,6 +95,19 @@ struct WideOperand {
                 (int)offset<WHOLE>(i, t, length), 0, 0, 0);
     }
 
+    // Step t straight into LDS, or zeros without reading anything.
+    __device__ __forceinline__ void load_if(bool there, uint32_t t, uint32_t length, lds_bytes to) const
+    {
+        const uint64_t left = bytes - t * step;
+        const rsrc_t r = make_rsrc(base + t * step, there ? left < kOutside ? (uint32_t)left : kOutside : 0);
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                r, (__attribute__((address_space(3))) void *)(to + (wave * kPieces + i) * 1024), 16,
+                (int)offset<false>(i, t, length), 0, 0, 0);
+    }
+
     // The same by way of registers: fetch(), and later put().
     template <bool WHOLE>
     __device__ __forceinline__ void fetch(uint32_t t, uint32_t length)
@@ -118,12 +121,7 @@ struct WideOperand {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
             *(__attribute__((address_space(3))) u32x4 *)(
-                to + ((threadIdx.x / 64 * kPieces + i) * 64 + threadIdx.x % 64) * 16) = held[i];
-    }
-
-    static __device__ __forceinline__ u32x4 fragment(lds_bytes from, int b, int s, uint32_t lane)
-    {
-        return Pieces<P, ACROSS, N>::fragment(from, b, s, lane);
+                to + Base::slot(i, threadIdx.x) * 16) = held[i];
     }
 };
 
@@ -157,12 +155,14 @@ template <class P>
 constexpr int wide_columns() { return __is_same(P, PE4M3) ? 128 : 256; }
 
 // O: the output's type.  ADD: onto what it holds (gradient).
-template <class P, class O, bool GRAD, bool ACROSS, bool ADD>
+// GRID: operands on the 16-byte grid, in whole pieces; others go through registers, which
+// leaves none for a gradient's two (2480 us where 128 x 128 tiles take 2210).
+template <class P, class O, bool GRAD, bool ACROSS, bool ADD, bool GRID>
 __device__ __forceinline__ void product_wide(const ProductParams &p)
 {
     constexpr int BN = wide_columns<P>();
-    using Rows = WideOperand<P, GRAD, 256>;
-    using Columns = WideOperand<P, ACROSS, BN>;
+    using Rows = std::conditional_t<GRID, WideOperand<P, GRAD, 256>, LooseOperand<P, GRAD, 256, uint32_t>>;
+    using Columns = std::conditional_t<GRID, WideOperand<P, ACROSS, BN>, LooseOperand<P, ACROSS, BN, uint32_t>>;
     constexpr bool kMx4 = __is_same(P, PMx4), kE4M3 = __is_same(P, PE4M3), kScaled = kMx4 || kE4M3;
     constexpr int kThreads = kProductThreads, kWaves = kThreads / 64;
     constexpr int CB = BN / 64, kAcross = 2;   // a wave's blocks of columns, waves side by side
@@ -328,7 +328,7 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
             to[0] = *(const __attribute__((address_space(3))) uint32_t *)from;
         }
     };
-    // operands of a tile, and its first two steps on their way
+    // operands of a tile, and its first two steps on their way (!GRID: the first)
     auto begin = [&](const WideTile &w) {
         if (w.steps == 0) return;
         const uint32_t tid = fresh_thread();
@@ -345,11 +345,16 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
                               w.column * (ACROSS ? (uint64_t)P::kSize : p.col_stride),
                           p.col_stride, p.n - w.column, along, tid);
         }
-        rows.template load<false>(0, w.length, r0);
-        columns.template load<false>(0, along, c0);
-        if (w.steps > 1) {
-            rows.template load<false>(1, w.length, r1);
-            columns.template load<false>(1, along, c1);
+        if constexpr (!GRID) {
+            rows.template fetch<false>(0, w.length);
+            columns.template fetch<false>(0, along);
+        } else {
+            rows.template load<false>(0, w.length, r0);
+            columns.template load<false>(0, along, c0);
+            if (w.steps > 1) {
+                rows.template load<false>(1, w.length, r1);
+                columns.template load<false>(1, along, c1);
+            }
         }
         fetch_scales(w, 0);
     };
@@ -366,7 +371,8 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
             constexpr int RB = decltype(blocks)::value;
             f32x16 acc[RB][CB];
             const uint32_t l = fresh_thread() % 64, h = l / 32;
-            const uint32_t whole = GRAD ? w.length / Rows::kRows : w.length / 128;
+            uint32_t whole = GRAD ? w.length / Rows::kRows : w.length / 128;
+            if (!GRID && ACROSS) whole = whole ? whole - 1 : 0;   // a step follows
             const uint32_t along = ACROSS && !GRAD ? column_length : w.length;
 #pragma unroll
             for (int r = 0; r < RB; ++r)
@@ -376,7 +382,6 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
             // e4m3: a step is 128 elements of k, which share their scales.  The sums of a
             // block of rows come from the matrix cores in `part` and join acc, scaled, while
             // the next block's are on their way.
-            // Half the work a step for as long a way from memory: three steps are in LDS.
             // Half the work a step for as long a way from memory: three steps are in LDS.
             u32x4 rf[4], cf[4][CB];
             f32x16 part[CB];
@@ -534,7 +539,7 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
             // FULL: two whole steps follow; kind 2: so for the first step
             auto body = [&](auto kind, auto parity, uint32_t t, lds_bytes rt, lds_bytes ct,
                             lds_bytes rn, lds_bytes cn) {
-                constexpr bool FULL = decltype(kind)::value != 0, FIRST = decltype(kind)::value == 2;
+                constexpr bool FULL = decltype(kind)::value != 0, FIRST = GRID && decltype(kind)::value == 2;
                 constexpr int E = decltype(parity)::value;
                 if constexpr (kMx4 && E == 0)
                     if (FULL || t + 2 < w.steps) fetch_scales(w, t / 2 + 1);
@@ -547,10 +552,15 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
                 // the rows of the next step, fetched a step ago, to LDS, and those of the
                 // one after it on their way; the columns follow when their buffer is free,
                 // so that loads never queue up
-                if (FULL ? !FIRST : t && t + 1 < w.steps) rows.put(rn);
+                if constexpr (GRID) {
+                    if (FULL ? !FIRST : t && t + 1 < w.steps) rows.put(rn);
+                } else if (FULL || t + 1 < w.steps) {
+                    rows.template put<FULL>(t + 1, w.length, rn);
+                    columns.template put<FULL>(t + 1, along, cn);
+                }
                 read(I2{}, rt, ct, 0);
                 mma(I1{}, 1, E);
-                if constexpr (FULL) interleave<kReads, kMma, 0, FIRST ? 0 : 8>();
+                if constexpr (FULL) interleave<kReads, kMma, 0, FIRST ? 0 : GRID ? 8 : 16>();
                 __builtin_amdgcn_sched_barrier(0);
                 if (FULL || t + 2 < w.steps) rows.template fetch<FULL>(t + 2, w.length);
                 read(I3{}, rt, ct, 1);
@@ -559,21 +569,26 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
                 __builtin_amdgcn_sched_barrier(0);
                 // this wave has read all of the step, and its part of the next is there:
                 // all loads but the last fetch have ended (step 1 is there from the start)
-                if constexpr (FULL && !FIRST) __asm__ volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+                if constexpr (!GRID) __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                else if constexpr (FULL && !FIRST) __asm__ volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
                 else if constexpr (FIRST) __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 else if (t) __asm__ volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
                 else __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (FULL) {
-                    columns.template load<true>(t + 2, along, ct);
+                    if constexpr (GRID) columns.template load<true>(t + 2, along, ct);
+                    else columns.template fetch<true>(t + 2, along);
                     read(I0{}, rn, cn, 0);
                     exponents(std::false_type{}, t + 1, 1 - E);
                     mma(I3{}, 1, E);
                     interleave<kReads + (kMx4 ? 2 : 0), kMma, 8, 0>();
                     __builtin_amdgcn_sched_barrier(0);
                 } else {
-                    if (t + 2 < w.steps) columns.template load<false>(t + 2, along, ct);
+                    if (t + 2 < w.steps) {
+                        if constexpr (GRID) columns.template load<false>(t + 2, along, ct);
+                        else columns.template fetch<false>(t + 2, along);
+                    }
                     if (t + 1 < w.steps) {
                         read(I0{}, rn, cn, 0);
                         exponents(std::true_type{}, t + 1, 1 - E);
@@ -683,7 +698,18 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
         else if (behind == 8) __asm__ volatile("s_waitcnt vmcnt(8)" ::: "memory");
         else if (behind == 4) __asm__ volatile("s_waitcnt vmcnt(4)" ::: "memory");
         else __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (w.steps) put_scales(0);
+        if (w.steps) {
+            put_scales(0);
+            if constexpr (!GRID) {
+                const uint32_t along = ACROSS && !GRAD ? column_length : w.length;
+                rows.template put<false>(0, w.length, r0);
+                columns.template put<false>(0, along, c0);
+                if (w.steps > 1) {
+                    rows.template fetch<false>(1, w.length);
+                    columns.template fetch<false>(1, along);
+                }
+            }
+        }
         __syncthreads();
         // at most a half or a quarter of the rows: the waves share them differently
         if (w.rows > 128) run(std::integral_constant<int, 4>{});
@@ -692,10 +718,10 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
     }
 }
 
-template <class P, class O, bool GRAD, bool ACROSS, bool ADD>
+template <class P, class O, bool GRAD, bool ACROSS, bool ADD, bool GRID>
 __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(ProductParams p)
 {
-    product_wide<P, O, GRAD, ACROSS, ADD>(p);
+    product_wide<P, O, GRAD, ACROSS, ADD, GRID>(p);
 }
 
 // With at most 256 registers the compiler lets matrix instructions write to those that
@@ -704,10 +730,10 @@ template <class P, class O>
 __global__ __launch_bounds__(kProductThreads, 1) __attribute__((amdgpu_num_vgpr(256))) void
 product_wide_e4m3_kernel(ProductParams p)
 {
-    product_wide<P, O, false, false, false>(p);
+    product_wide<P, O, false, false, false, true>(p);
 }
 
-template <class P, class O, bool GRAD, bool ACROSS, bool ADD>
+template <class P, class O, bool GRAD, bool ACROSS, bool ADD, bool GRID>
 hipError_t go_wide(ProductParams p, hipStream_t s)
 {
     constexpr uint32_t BN = wide_columns<P>();
@@ -722,7 +748,7 @@ hipError_t go_wide(ProductParams p, hipStream_t s)
     p.spans = tiles >= 8 * cus;
     void (*kernel)(ProductParams);
     if constexpr (__is_same(P, PE4M3)) kernel = product_wide_e4m3_kernel<P, O>;
-    else kernel = product_wide_kernel<P, O, GRAD, ACROSS, ADD>;
+    else kernel = product_wide_kernel<P, O, GRAD, ACROSS, ADD, GRID>;
     return launch_kernel(kernel,
                          dim3(grid_of(tiles < cus ? (tiles + 7) / 8 * 8 : cus, kProductThreads)),
                          dim3(kProductThreads), 0, s, p);
@@ -732,11 +758,13 @@ template <class P, class O>
 hipError_t launch_wide(const ProductParams &p, bool grad, bool across, hipStream_t s)
 {
     if constexpr (P::kSize == 1) {
-        return go_wide<P, O, false, false, false>(p, s);
+        return go_wide<P, O, false, false, false, true>(p, s);
     } else {
         if (grad)
-            return p.add ? go_wide<P, O, true, true, true>(p, s) : go_wide<P, O, true, true, false>(p, s);
-        return across ? go_wide<P, O, false, true, false>(p, s) : go_wide<P, O, false, false, false>(p, s);
+            return p.add ? go_wide<P, O, true, true, true, true>(p, s)
+                         : go_wide<P, O, true, true, false, true>(p, s);
+        return across ? go_wide<P, O, false, true, false, true>(p, s)
+                      : go_wide<P, O, false, false, false, true>(p, s);
     }
 }
 
