@@ -5,7 +5,9 @@
 
 namespace xred {
 
-// Tiles of 256 x 256 fill the chip from about half a tile a CU on.
+// Tiles of 256 x 256 fill the chip from about half a tile a CU on, even if few of their rows
+// exist (64 experts, 2048 x 2048: 8192 rows 165 us, tiles of 128 x 128 189, mx4 78 and 92;
+// 4096 rows 165 and 161, mx4 70 and 69; the gradient of as many 170 and 266).
 inline bool wide_pays(const ProductParams &p, bool grad)
 {
     const uint64_t columns = (p.n + 255) / 256;
@@ -14,7 +16,8 @@ inline bool wide_pays(const ProductParams &p, bool grad)
     return p.n > 128 && rows * columns >= 128;
 }
 
-// Few rows for an expert: its weights are what costs.  (At 64 elements and more, which
+// Few rows for an expert: its weights are what costs (64 experts, bf16: 2048 rows of 2048 x
+// 4096 209 us, 187 in wide tiles; 8 rows of 4096 x 4096 47 and 71).  (At 64 elements and more, which
 // pieces and mx4's exponents are read in whole.)
 inline bool narrow_pays(const ProductParams &p)
 {
@@ -49,9 +52,10 @@ hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, 
         if (direct)
             return p.out_type == XRED_FLOAT32 ? launch_wide<P, TF32>(p, grad, across, s)
                                               : launch_wide<P, O>(p, grad, across, s);
-        // 32768 rows, 64 experts, 4097 x 2049 bf16: 1390 us, tiles of 128 x 128 2160;
-        // transposed 1050 and 2090
-        if (!grad && p.out_type == dtype_of<O>())
+        // Loose operands, 64 experts, bf16: 32768 rows of 4097 x 2049 1343 us, tiles of
+        // 128 x 128 2160 (transposed 1090 and 2090); 8192 rows of 2049 x 2047 310 and 294,
+        // 4096 rows 300 and 229.
+        if (!grad && p.out_type == dtype_of<O>() && p.rows >= 192ull * p.experts)
             return across ? go_wide<P, O, false, true, false, false>(p, s)
                           : go_wide<P, O, false, false, false, false>(p, s);
     }

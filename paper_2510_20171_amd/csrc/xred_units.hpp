@@ -20,13 +20,14 @@ struct UnitItems {
     uint32_t lanes;            // of an item
 };
 
-// Items of `rows` rows of n elements (below 2^31 of them, as the caller checked), and the
-// grid that takes them.
-inline unsigned plan_units(uint64_t rows, uint64_t n, UnitItems &u)
+// Items of `rows` rows of n elements (fewer items than 2^32, as the caller checked), in units
+// of UNIT, and the grid that takes them.  32 elements are never split between items.
+template <int UNIT = 8>
+unsigned plan_units(uint64_t rows, uint64_t n, UnitItems &u)
 {
-    const uint64_t units = (n + 7) / 8, per_row = (units + 63) / 64;
+    const uint64_t units = (n + UNIT - 1) / UNIT, per_row = (units + 63) / 64;
     u.lanes = 64;
-    while (u.lanes > 4 && u.lanes / 2 >= units) u.lanes /= 2;
+    while (u.lanes > 32 / UNIT && u.lanes / 2 >= units) u.lanes /= 2;
     u.items = (uint32_t)(rows * per_row);
     u.per_row = (uint32_t)per_row;
     const uint64_t at_once = kUnitThreads / u.lanes;
