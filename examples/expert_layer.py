@@ -5,9 +5,11 @@ reduction of one layer's partial sums and the next.
 
 ``serve`` is the inference form with 8-bit expert inputs, for any number of
 tokens from one; ``train_step`` the same layer in bf16 with its backward pass,
-the library's gradients behind torch.autograd.Function.  The products (router
-and experts) are torch's; everything between them is the library's.  Run as a
-program, it checks both against the layer written in plain torch and times them.
+the library's gradients behind torch.autograd.Function.  The router's product is
+torch's; everything else is the library's.  ``GatedLayer`` has experts of two
+products with a gated activation between them; ``serve_gated`` runs it with its
+weights in 8 or 4 bits.  Run as a program, it checks both forms of the plain layer
+against torch and times them all.
 """
 from __future__ import annotations
 
@@ -39,14 +41,86 @@ class Layer:
         self.expert = new(experts, hidden, hidden, scale=hidden ** -0.5)
 
 
-def products(rows, expert, offsets):
+    def weights(self):
+        return [self.expert]
+
+    def apply(self, rows, offsets):
+        return Products.apply(rows, self.expert, offsets)
+
+
+class GatedLayer(Layer):
+    """Experts of two products: rows of 2 * width gates and values, of which the gated
+    activation makes `width`, and back."""
+
+    def __init__(self, hidden, width, experts, topk, dtype=torch.bfloat16, device="cuda", seed=0):
+        super().__init__(hidden, experts, topk, dtype, device, seed)
+        g = torch.Generator(device=device).manual_seed(seed + 1)
+        new = lambda *shape: torch.empty(shape, device=device).normal_(
+            0, shape[-1] ** -0.5, generator=g).to(dtype)
+        self.width = width
+        self.up, self.down = new(experts, 2 * width, hidden), new(experts, hidden, width)
+
+    def weights(self):
+        return [self.up, self.down]
+
+    def apply(self, rows, offsets):
+        gated = Gate.apply(Products.apply(rows, self.up, offsets), offsets)
+        return Products.apply(gated, self.down, offsets)
+
+
+class Products(torch.autograd.Function):
     """Each expert's product with its rows, which lie together; rows past the last stay 0."""
-    out = []
-    at = offsets.tolist()   # the host needs the sizes: torch has no product over ranges on the GPU
-    for e in range(len(expert)):
-        out.append(rows[at[e]:at[e + 1]] @ expert[e].t())
-    out.append(rows.new_zeros((rows.shape[0] - at[-1], rows.shape[1])))
-    return torch.cat(out)
+
+    @staticmethod
+    def forward(ctx, rows, weight, offsets):
+        out = rows.new_zeros((rows.shape[0], weight.shape[1]))
+        xr.group_product(rows, weight, offsets, out)
+        ctx.save_for_backward(rows, weight, offsets)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        rows, weight, offsets = ctx.saved_tensors
+        dout = dout.contiguous()
+        drows, dweight = torch.zeros_like(rows), torch.empty_like(weight)
+        xr.group_product(dout, weight, offsets, drows, transpose=True)
+        xr.group_product_grad(dout, rows, offsets, dweight)
+        return drows, dweight, None
+
+
+class Gate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, offsets):
+        out = x.new_zeros((x.shape[0], x.shape[1] // 2))
+        xr.gate(x, out, offsets=offsets)
+        ctx.save_for_backward(x, offsets)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        x, offsets = ctx.saved_tensors
+        dx = torch.zeros_like(x)
+        xr.gate_grad(dout.contiguous(), x, dx, offsets=offsets)
+        return dx, None
+
+
+def to_e4m3(w):
+    """Weights in 8 bits with a scale for every 128 x 128 of them."""
+    e, n, k = w.shape
+    by = torch.nn.functional.pad(w.float(), (0, -k % GROUP, 0, -n % GROUP)).unflatten(
+        2, (-1, GROUP)).unflatten(1, (-1, GROUP))
+    scale = by.abs().amax((2, 4), keepdim=True).clamp(min=2.0 ** -100) / 448
+    w8 = (by / scale).to(torch.float8_e4m3fn).flatten(3).flatten(1, 2)[:, :n, :k].contiguous()
+    return w8, scale[:, :, 0, :, 0].contiguous()
+
+
+def to_mx4(w):
+    """Weights in 4 bits with a power of two for every 32 of a row."""
+    e, n, k = w.shape
+    w4 = torch.empty((e, n, -(-k // 32) * 16), dtype=torch.uint8, device=w.device)
+    scale = torch.empty((e, n, -(-k // 32)), dtype=torch.uint8, device=w.device)
+    xr.quant_mx4(w.flatten(0, 1), w4.flatten(0, 1), scale.flatten(0, 1))
+    return w4, scale
 
 
 def plan(ids, experts):
@@ -55,6 +129,15 @@ def plan(ids, experts):
     pos = torch.empty_like(ids)
     xr.dispatch_plan(ids, counts, offsets, pos)
     return counts, offsets, pos
+
+
+def routed(layer, y):
+    """Weights of the tokens' experts, where the experts' rows begin, and the slots' rows."""
+    ids = torch.empty((y.shape[0], layer.topk), dtype=torch.int32, device=y.device)
+    weights = torch.empty(ids.shape, device=y.device)
+    xr.route(y @ layer.router.t(), ids, weights, score="sigmoid", bias=layer.bias, scale=SCALE)
+    _, offsets, pos = plan(ids, layer.experts)
+    return weights, offsets, pos
 
 
 def serve(layer, partial_sums, stream_in):
@@ -67,16 +150,48 @@ def serve(layer, partial_sums, stream_in):
     scale = torch.empty((tokens, -(-hidden // GROUP)), device=dev)
     xr.fold_norm(partial_sums, y, residual=stream_in, weight=layer.norm, sum=h, out8=y8,
                  scale=scale, group=GROUP)
-    ids = torch.empty((tokens, k), dtype=torch.int32, device=dev)
-    weights = torch.empty((tokens, k), device=dev)
-    xr.route(y @ layer.router.t(), ids, weights, score="sigmoid", bias=layer.bias, scale=SCALE)
-    _, offsets, pos = plan(ids, layer.experts)
+    weights, offsets, pos = routed(layer, y)
     rows8 = torch.empty((tokens * k, hidden), dtype=torch.float8_e4m3fn, device=dev)
     row_scale = torch.empty((tokens * k, scale.shape[1]), device=dev)
     xr.dispatch(y8, pos, rows8, scale=scale, out_scale=row_scale)
     rows = rows8.float() * row_scale.repeat_interleave(GROUP, 1)[:, :hidden]
     out = torch.empty_like(h)
-    xr.combine(products(rows.to(dt), layer.expert, offsets), pos, out, weights=weights, base=h)
+    xr.combine(layer.apply(rows.to(dt), offsets), pos, out, weights=weights, base=h)
+    return out
+
+
+def serve_gated(layer, weights4or8, partial_sums, stream_in):
+    """A GatedLayer with (up, its scales, down, its scales) from to_e4m3 or to_mx4: rows go
+    through both products in as many bits."""
+    (up, up_scale), (down, down_scale) = weights4or8
+    tokens, hidden, dt, dev = stream_in.shape[0], layer.hidden, stream_in.dtype, stream_in.device
+    slots, mx4 = tokens * layer.topk, up.dtype == torch.uint8
+    new = lambda rows, columns, dtype: torch.empty((rows, columns), dtype=dtype, device=dev)
+    h, y = torch.empty_like(stream_in), torch.empty_like(stream_in)
+    inner, outer = new(slots, 2 * layer.width, dt), new(slots, hidden, dt)
+    out = torch.empty_like(h)
+    if mx4:
+        xr.fold_norm(partial_sums, y, residual=stream_in, weight=layer.norm, sum=h)
+        weights, offsets, pos = routed(layer, y)
+        rows, gated = torch.zeros_like(outer), new(slots, layer.width, dt)
+        xr.dispatch(y, pos, rows)
+        rows4, scale = to_mx4(rows[None])
+        xr.group_product(rows4[0], up, offsets, inner, scale=scale[0], w_scale=up_scale)
+        xr.gate(inner, gated, offsets=offsets)
+        gated4, scale = to_mx4(gated[None])
+        xr.group_product(gated4[0], down, offsets, outer, scale=scale[0], w_scale=down_scale)
+    else:
+        y8, y_scale = new(tokens, hidden, up.dtype), new(tokens, up_scale.shape[2], torch.float32)
+        xr.fold_norm(partial_sums, y, residual=stream_in, weight=layer.norm, sum=h, out8=y8,
+                     scale=y_scale, group=GROUP)
+        weights, offsets, pos = routed(layer, y)
+        rows8, scale = new(slots, hidden, up.dtype), new(slots, up_scale.shape[2], torch.float32)
+        xr.dispatch(y8, pos, rows8, scale=y_scale, out_scale=scale)
+        xr.group_product(rows8, up, offsets, inner, scale=scale, w_scale=up_scale)
+        gated8, scale = new(slots, layer.width, up.dtype), new(slots, down_scale.shape[2], torch.float32)
+        xr.gate(inner, out8=gated8, scale=scale, group=GROUP, offsets=offsets)
+        xr.group_product(gated8, down, offsets, outer, scale=scale, w_scale=down_scale)
+    xr.combine(outer, pos, out, weights=weights, base=h)
     return out
 
 
@@ -154,14 +269,14 @@ def forward(layer, partial_sums, stream_in):
     h, y = FoldNorm.apply(stream_in, layer.norm, *partial_sums)
     ids, weights = Route.apply(y @ layer.router.t(), layer.bias, layer.topk)
     _, offsets, pos = plan(ids, layer.experts)
-    rows = products(Dispatch.apply(y, pos), layer.expert, offsets)
+    rows = layer.apply(Dispatch.apply(y, pos), offsets)
     return Combine.apply(rows, pos, weights, h)
 
 
 def train_step(layer, partial_sums, stream_in, dout):
     """Output and the gradients of the input stream, of every weight and (all alike) of
     the partial sums."""
-    leaves = [stream_in, layer.norm, layer.router, layer.expert, partial_sums[0]]
+    leaves = [stream_in, layer.norm, layer.router, *layer.weights(), partial_sums[0]]
     for t in leaves:
         t.requires_grad_(True)
         t.grad = None
@@ -217,8 +332,13 @@ def main():
     print("train_step: off by %.4f of the output" % off(out, plain(layer, sums, x, ids, False)))
     for name, grad in zip(("stream", "norm", "router", "experts", "partial sums"), grads):
         print("  gradient of the %s: norm %.4g" % (name, float(grad.float().norm())))
+    gated = GatedLayer(a.hidden, a.hidden, a.experts, a.topk)
+    eight, four = ([to(w) for w in gated.weights()] for to in (to_e4m3, to_mx4))
     for what, f in (("serve", lambda: serve(layer, sums, x)),
-                    ("train_step", lambda: train_step(layer, sums, x, dout))):
+                    ("train_step", lambda: train_step(layer, sums, x, dout)),
+                    ("serve_gated, e4m3", lambda: serve_gated(gated, eight, sums, x)),
+                    ("serve_gated, mx4", lambda: serve_gated(gated, four, sums, x)),
+                    ("train_step, gated", lambda: train_step(gated, sums, x, dout))):
         f()
         torch.cuda.synchronize()
         t = time.perf_counter()
