@@ -373,7 +373,8 @@ struct RowTiles {
         for (int j = 0; j < kEach; ++j) first[j] += before;
     }
 
-    // Tile t (below total): its expert and rows [lo, hi), into found[3] (LDS).
+    // Tile t (below total): its expert and rows [lo, hi), into found[3] (LDS).  Offsets that do
+    // not ascend can make total overflow, and then none is found.
     __device__ __forceinline__ void find(uint32_t t, uint32_t rows_of_tile, uint32_t *found) const
     {
         __syncthreads();   // the tile before has been read
@@ -464,6 +465,7 @@ __global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kern
     if constexpr (GRAD) {
         total = share ? p.experts * share * 8 : p.experts * of_expert;
     } else {
+        if (threadIdx.x < 3) found[threadIdx.x] = 0;
         all.start(p, shared, [](uint32_t n) { return (n + BM - 1) / BM; });
         total = all.total * p.col_tiles;
     }
@@ -492,6 +494,7 @@ __global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kern
             e = found[0];
             m0 = found[1];
             items = found[2] - m0;
+            if (items == 0) continue;
             n0 = rest / high * BN;
             length = p.k * P::kSize;
             from = p.row + m0 * p.row_stride;

@@ -1,21 +1,34 @@
 // xred_product_wide.hpp -- the experts' products in tiles of 256 x 256, for calls with
 // enough rows to fill the chip with them.
 //
+// Bound by the matrix cores (32768 rows of 64 experts, 4096 x 2048 bf16: 0.55 TFLOP, 390 us at
+// a large library product's rate, 613 here; one expert 1217 TFLOP/s; 128 x 128 tiles 1340 us).
+//
 // A workgroup of four waves has a CU to itself: each wave keeps 128 x 128 sums in its
 // 256 accumulation registers, so that a fragment of either operand is used four times
 // and LDS is read at half of its rate while the matrix cores run.  Two steps of k (128
-// KB) are in LDS, one being multiplied, the next on its way by loads straight to LDS; a
-// step's buffer is free once its last fragments are read, three quarters through it, and
-// is filled again at once.  Fragments are read one sub-step ahead, one between every two
-// matrix instructions.
+// KB) are in LDS, one being multiplied, the next on its way: its columns by loads straight
+// to LDS, into a buffer that is free once the step's last fragments are read, three quarters
+// through it, its rows through registers, so that loads spread over the step (all straight
+// to LDS: they queue up behind one another).  Fragments are read one sub-step ahead, one
+// between every two matrix instructions.
 //
 // Buffer descriptors bound every load: what lies past the operand's rows, columns or k
 // comes as zero, so ragged tiles run the same code.  A tile of at most 128 or 64 rows
 // has a main loop of its own that does a half or a quarter of the products.
 //
+// mx4: exponents of two steps at a time lie in LDS beside the operands, each lane's own
+// dword of four (32768 rows, 4096 x 4096: 430 us, 2.6 PFLOP/s; 128 x 128 tiles 1100).
+//
+// e4m3: a step is the 128 elements that share their scales.  Its sums are scaled by vector
+// instructions, 16 for two matrix instructions, and join sums of binary32: a tile of 256 x
+// 128 leaves registers for them, and three steps in LDS since each is half the work for as
+// long a way from memory (29500 rows, 4096 x 4096: 843 us, 1.17 PFLOP/s; two steps and 256
+// x 128 1070, 128 x 128 tiles 1196).
+//
 // Workgroups stay for several tiles.  The first two steps of the next tile are loaded
-// before the results of the last one go out, through LDS (32 KB beside the operands'), in
-// whole 128-byte pieces of rows.
+// before the results of the last one go out, through LDS beside the operands', in whole
+// pieces of 128 bytes of rows (mx4: 64).
 #pragma once
 
 #include "xred_product.hpp"
@@ -185,6 +198,10 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
     // rows as take about as long, two or three if those rows are at most 128 or 64.
     auto span = [&](uint32_t rest) { return p.spans ? rest > 64 ? 2u : 3u : 1u; };
     auto whole_tiles = [](uint32_t n) { return n / 256 + (n % 256 > 128); };
+    auto items_of = [&](uint32_t n) {   // of an expert with n rows
+        const uint32_t rest = n % 256, s = span(rest);
+        return whole_tiles(n) * p.col_tiles + (rest == 0 || rest > 128 ? 0 : (p.col_tiles + s - 1) / s);
+    };
     uint32_t total;   // items
     // gradient: an expert's tiles are dealt to all XCDs where there are enough of them,
     // since experts' rows, and with them the tiles' lengths, differ
@@ -193,11 +210,7 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
         total = share ? p.experts * share * 8 : p.experts * of_expert;
     } else {
         RowTiles<kThreads> all;
-        all.start(p, (uint32_t *)stage, [&](uint32_t n) {
-            const uint32_t rest = n % 256, s = span(rest);
-            return whole_tiles(n) * p.col_tiles +
-                   (rest == 0 || rest > 128 ? 0 : (p.col_tiles + s - 1) / s);
-        });
+        all.start(p, (uint32_t *)stage, items_of);
 #pragma unroll
         for (int j = 0; j < RowTiles<kThreads>::kEach; ++j)
             first[threadIdx.x * RowTiles<kThreads>::kEach + j] = all.first[j];
@@ -238,20 +251,22 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
             w.length = hi - lo;
             w.steps = (w.length + Rows::kRows - 1) / Rows::kRows;
         } else {
-            uint32_t i;
+            const uint32_t l = fresh_thread() % 64;
+            uint32_t i, lo, hi, row, column;
             for (;; place += gridDim.x) {
                 if (place / 8 >= (total + 7) / 8) return false;
-                if (tile_of(place, total, i)) break;
+                if (!tile_of(place, total, i)) continue;
+                uint32_t upto = 0;   // experts whose first item is i or before
+                for (uint32_t e = 0; e < p.experts; e += 64)
+                    upto += __popcll(__builtin_amdgcn_ballot_w64(e + l < p.experts && first[e + l] <= i));
+                if (upto == 0) continue;
+                w.expert = __builtin_amdgcn_readfirstlane(upto - 1);
+                i -= __builtin_amdgcn_readfirstlane(first[w.expert]);
+                uniform_rows(p, w.expert, lo, hi);
+                // else offsets do not ascend, and total has overflowed
+                if (i < items_of(hi - lo)) break;
             }
             place += gridDim.x;
-            const uint32_t l = fresh_thread() % 64;
-            uint32_t upto = 0;   // experts whose first item is i or before
-            for (uint32_t e = 0; e < p.experts; e += 64)
-                upto += __popcll(__builtin_amdgcn_ballot_w64(e + l < p.experts && first[e + l] <= i));
-            w.expert = __builtin_amdgcn_readfirstlane(upto - 1);
-            i -= __builtin_amdgcn_readfirstlane(first[w.expert]);
-            uint32_t lo, hi, row, column;
-            uniform_rows(p, w.expert, lo, hi);
             const uint32_t whole = whole_tiles(hi - lo);
             if (i < whole * p.col_tiles) {
                 grouped(i, whole, p.col_tiles, row, column);
