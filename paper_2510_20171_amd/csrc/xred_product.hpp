@@ -624,30 +624,56 @@ __global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kern
             }
         }
         char *out = p.out + (GRAD ? e * p.out_expert : 0) + m0 * p.out_stride;
+        auto leave = [&](uint32_t row, uint32_t col, float (&v)[4]) {
+            if (row >= items || col >= p.n) return;
+            char *to = out + row * p.out_stride;
+            const uint32_t n = p.n - col < 4 ? p.n - col : 4;
+            if (GRAD && p.add)
 #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const uint32_t row = (wr * RB + r) * 32 + l % 32;
-            if (row < items) {
-                char *to = out + row * p.out_stride;
+                for (uint32_t j = 0; j < 4; ++j)
+                    if (j < n) v[j] += value_at(to, col + j, p.out_type);
+            store_four(to, col, n, v, p.out_type);
+        };
+        // Results of the larger tiles leave through LDS, a wave's 32 x 32 at a time in a part of
+        // the first step's buffer, so that a store has 8 lanes' 4 columns of a row side by side
+        // and not 2 (gradient of 4097 x 2049 bf16, 32768 rows: 1745 to 1540 us; the smaller ones
+        // and e4m3, short of registers, lose 5 to 10 % by it).  A wave's accesses to LDS happen
+        // in order.
+        constexpr bool STAGED = RB == 2 && !__is_same(P, PE4M3);
+        const lds_bytes stage = r0 + wave * 4096;
 #pragma unroll
-                for (int c = 0; c < CB; ++c)
+        for (int r = 0; r < RB; ++r)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint32_t col = n0 + (wc * CB + c) * 32 + 8 * q + 4 * h;
-                        if (col < p.n) {
-                            const uint32_t n = p.n - col < 4 ? p.n - col : 4;
-                            float v[4];
+            for (int c = 0; c < CB; ++c) {
+                const uint32_t row0 = (wr * RB + r) * 32, col0 = n0 + (wc * CB + c) * 32;
+                if constexpr (STAGED) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) v[j] = acc[r][c][4 * q + j];
-                            if (GRAD && p.add)
+                    for (int q = 0; q < 4; ++q)
+                        *(__attribute__((address_space(3))) u32x4 *)(
+                            stage + l % 32 * 128 + ((2 * q + h) ^ l % 8) * 16) =
+                            u32x4{__float_as_uint(acc[r][c][4 * q]), __float_as_uint(acc[r][c][4 * q + 1]),
+                                  __float_as_uint(acc[r][c][4 * q + 2]), __float_as_uint(acc[r][c][4 * q + 3])};
+                    __builtin_amdgcn_wave_barrier();
+                }
 #pragma unroll
-                                for (uint32_t j = 0; j < 4; ++j)
-                                    if (j < n) v[j] += value_at(to, col + j, p.out_type);
-                            store_four(to, col, n, v, p.out_type);
-                        }
+                for (uint32_t q = 0; q < 4; ++q) {
+                    float v[4];
+                    if constexpr (STAGED) {
+                        const uint32_t row = q * 8 + l / 8;
+                        const u32x4 x = *(const __attribute__((address_space(3))) u32x4 *)(
+                            stage + row * 128 + (l % 8 ^ row % 8) * 16);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(x[j]);
+                        leave(row0 + row, col0 + l % 8 * 4, v);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = acc[r][c][4 * q + j];
+                        leave(row0 + l % 32, col0 + 8 * q + 4 * h, v);
                     }
+                }
+                if constexpr (STAGED) __builtin_amdgcn_wave_barrier();
             }
-        }
+        if constexpr (STAGED) __syncthreads();   // the next tile's first step goes there
     }
 }
 
