@@ -139,7 +139,7 @@ def _row_count(offsets, device):
     n = offsets.numel()
     if n < 1:
         _refuse("offsets is empty")
-    return _ints(offsets, n, "offsets", device) + 4 * (n - 1)
+    return ctypes.c_void_p(_ints(offsets, n, "offsets", device).value + 4 * (n - 1))
 
 
 def gate(x, out=None, *, out8=None, scale=None, group: int = 128, offsets=None,
