@@ -7,31 +7,47 @@ namespace xred {
 
 // Tiles of 256 x 256 fill the chip from about half a tile a CU on, even if few of their rows
 // exist (64 experts, 2048 x 2048: 8192 rows 165 us, tiles of 128 x 128 189, mx4 78 and 92;
-// 4096 rows 165 and 161, mx4 70 and 69; the gradient of as many 170 and 266).
-inline bool wide_pays(const ProductParams &p, bool grad)
+// 4096 rows 165 and 161, mx4 70 and 69; the gradient of as many 170 and 266).  fp32, whose
+// matrix instructions take eight times as long, keeps smaller tiles as busy and loses more by
+// rows that do not exist: 32768 rows of 4096 x 1024 2130 and 2390, but 8192 of 2048 x 2048
+// 1133 and 895 and the gradient of 32768 2630 and 2380.
+inline bool wide_pays(const ProductParams &p, bool grad, bool f32)
 {
     const uint64_t columns = (p.n + 255) / 256;
     const uint64_t rows = grad ? (uint64_t)p.experts * ((p.m + 255) / 256)
                                : p.rows / 256 + (p.rows < p.experts ? p.rows : p.experts);
+    if (f32 && (grad || p.rows < 256ull * p.experts || rows * columns < 1024)) return false;
     return p.n > 128 && rows * columns >= 128;
 }
 
-// Few rows for an expert: its weights are what costs (64 experts, bf16: 2048 rows of 2048 x
-// 4096 209 us, 187 in wide tiles; 8 rows of 4096 x 4096 47 and 71).  (At 64 elements and more, which
-// pieces and mx4's exponents are read in whole.)
+// Few rows for an expert: its weights are what costs (64 experts, bf16: 8 rows of 4096 x 4096
+// 47 us, 71 in 128 x 128 tiles; 2048 rows of 2048 x 4096 209, in wide tiles 187).  And where
+// larger tiles would leave CUs without one, more of them with more steps on their way (one
+// expert, 220 rows of 299 x 2045: 14.7 us, in 64 x 64 tiles 23.8; 2048 x 4096 18.5 and 24.8;
+// 64 experts, 2048 rows of 299 x 2045 23 and 38; from 64 x 64 tiles for every CU on it turns:
+// 8 experts, 2000 rows of 640 x 320 7.8 and 6.2).  At 64 elements and more, which pieces and
+// mx4's exponents are read in whole.
 inline bool narrow_pays(const ProductParams &p)
 {
-    return p.rows <= 16ull * p.experts && p.n >= 64 && p.k >= 64 && p.row_stride < kWideStride && p.col_stride < kWideStride;
+    if (p.n < 64 || p.k < 64) return false;
+    const uint64_t tiles = (p.rows / 64 + (p.rows < p.experts ? p.rows : p.experts)) * (uint64_t)((p.n + 63) / 64);
+    const uint64_t cus = device_cus();
+    return (p.rows <= 16ull * p.experts || tiles <= cus || (p.rows <= 32ull * p.experts && tiles < 2 * cus)) &&
+           p.row_stride < kWideStride && p.col_stride < kWideStride;
 }
 
-// Tiles of 64 x 64 where there are too few of 128 x 128 to keep the chip busy.
+// Tiles of 64 x 64 where there are too few of 128 x 128 to keep the chip busy, and in fp32,
+// bound by its matrix instructions, where experts would leave most of 128 rows empty (64
+// experts, 4096 rows of 2048 x 2048: 526 us, 643 in 128 x 128 tiles).
 template <class P, bool GRAD, bool ACROSS, bool DIRECT>
 hipError_t go_tiles(const ProductParams &p, hipStream_t s)
 {
     const uint64_t rows = GRAD ? (uint64_t)p.experts * ((p.m + 127) / 128)
                                : p.rows / 128 + (p.rows < p.experts ? p.rows : p.experts);
-    return rows * ((p.n + 127) / 128) < 2 * device_cus() ? go_product<P, GRAD, ACROSS, DIRECT, 1, 1>(p, s)
-                                                        : go_product<P, GRAD, ACROSS, DIRECT, 2, 2>(p, s);
+    const bool small = (P::kSize == 4 && !GRAD && p.rows < 96ull * p.experts) ||
+                       rows * ((p.n + 127) / 128) < 2 * device_cus();
+    return small ? go_product<P, GRAD, ACROSS, DIRECT, 1, 1>(p, s)
+                 : go_product<P, GRAD, ACROSS, DIRECT, 2, 2>(p, s);
 }
 
 template <class P>
@@ -47,7 +63,7 @@ hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, 
             return direct ? go_narrow<P, true, true>(p, s) : go_narrow<P, true, false>(p, s);
         return direct ? go_narrow<P, false, true>(p, s) : go_narrow<P, false, false>(p, s);
     }
-    if (p.row_stride < kWideStride && p.col_stride < kWideStride && wide_pays(p, grad)) {
+    if (p.row_stride < kWideStride && p.col_stride < kWideStride && wide_pays(p, grad, es == 4)) {
         using O = typename OwnType<P>::T;
         if (direct)
             return p.out_type == XRED_FLOAT32 ? launch_wide<P, TF32>(p, grad, across, s)
@@ -84,7 +100,7 @@ hipError_t launch_product_scaled(const ProductParams &p, hipStream_t s)
     if (narrow_pays(p))
         return direct ? go_narrow<P, false, true>(p, s) : go_narrow<P, false, false>(p, s);
     if (direct && p.row_stride < kWideStride && p.col_stride < kWideStride && scale_words<P>(p) &&
-        wide_pays(p, false))
+        wide_pays(p, false, false))
         return p.out_type == XRED_FLOAT32    ? launch_wide<P, TF32>(p, false, false, s)
                : p.out_type == XRED_BFLOAT16 ? launch_wide<P, TBF16>(p, false, false, s)
                                              : launch_wide<P, TF16>(p, false, false, s);

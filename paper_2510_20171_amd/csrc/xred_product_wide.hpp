@@ -163,7 +163,8 @@ __device__ __forceinline__ void uniform_rows(const ProductParams &p, uint32_t e,
 }
 
 // Columns of a tile.  e4m3's sums are scaled by vector instructions, which cannot reach
-// the accumulation registers: half as many fit beside what else a wave holds.
+// the accumulation registers: half as many fit beside what else a wave holds.  (Its file
+// is compiled so that matrix instructions write to the others too.)
 template <class P>
 constexpr int wide_columns() { return __is_same(P, PE4M3) ? 128 : 256; }
 
@@ -739,15 +740,6 @@ __global__ __launch_bounds__(kProductThreads, 1) void product_wide_kernel(Produc
     product_wide<P, O, GRAD, ACROSS, ADD, GRID>(p);
 }
 
-// With at most 256 registers the compiler lets matrix instructions write to those that
-// vector instructions read; with more, to the others, each value moved before it is used.
-template <class P, class O>
-__global__ __launch_bounds__(kProductThreads, 1) __attribute__((amdgpu_num_vgpr(256))) void
-product_wide_e4m3_kernel(ProductParams p)
-{
-    product_wide<P, O, false, false, false, true>(p);
-}
-
 template <class P, class O, bool GRAD, bool ACROSS, bool ADD, bool GRID>
 hipError_t go_wide(ProductParams p, hipStream_t s)
 {
@@ -761,10 +753,7 @@ hipError_t go_wide(ProductParams p, hipStream_t s)
     // even out what workgroups do where each has enough items (12 a CU: 678 us without, 653
     // with; 6 a CU: 755 and 892, an item more or less being a fifth of the time)
     p.spans = tiles >= 8 * cus;
-    void (*kernel)(ProductParams);
-    if constexpr (__is_same(P, PE4M3)) kernel = product_wide_e4m3_kernel<P, O>;
-    else kernel = product_wide_kernel<P, O, GRAD, ACROSS, ADD, GRID>;
-    return launch_kernel(kernel,
+    return launch_kernel(product_wide_kernel<P, O, GRAD, ACROSS, ADD, GRID>,
                          dim3(grid_of(tiles < cus ? (tiles + 7) / 8 * 8 : cus, kProductThreads)),
                          dim3(kProductThreads), 0, s, p);
 }
@@ -775,9 +764,10 @@ hipError_t launch_wide(const ProductParams &p, bool grad, bool across, hipStream
     if constexpr (P::kSize == 1) {
         return go_wide<P, O, false, false, false, true>(p, s);
     } else {
-        if (grad)
-            return p.add ? go_wide<P, O, true, true, true, true>(p, s)
-                         : go_wide<P, O, true, true, false, true>(p, s);
+        if constexpr (P::kSize == 2)
+            if (grad)
+                return p.add ? go_wide<P, O, true, true, true, true>(p, s)
+                             : go_wide<P, O, true, true, false, true>(p, s);
         return across ? go_wide<P, O, false, true, false, true>(p, s)
                       : go_wide<P, O, false, false, false, true>(p, s);
     }

@@ -68,6 +68,15 @@ def test_tiles_of_few_rows_side_by_side(xr, dtype):
     run(xr, g, TYPES[dtype], counts, 5, 6664, 136)
 
 
+@pytest.mark.parametrize("transpose", [False, True], ids=["nk", "kn"])
+@pytest.mark.parametrize("n", [26248, 26245])
+def test_many_rows_and_columns_f32(xr, n, transpose):
+    """fp32 takes tiles of 256 x 256 where there are a thousand of them."""
+    g = generator(13)
+    for k, pad, off in ((8, 0, 0), (72, 8, 8), (160, 0, 0), (33, 0, 0), (131, 3, 1)):
+        run(xr, g, torch.float32, [1300, 801], 3, n, k, transpose, pad, off)
+
+
 @pytest.mark.parametrize("n", WIDE_N)
 @pytest.mark.parametrize("out_dtype", TYPES)
 def test_many_rows_e4m3(xr, out_dtype, n):

@@ -5,7 +5,7 @@ import re
 
 from test_kernel_resources import code_objects, kernels  # noqa: F401 (fixtures)
 
-NEW = re.compile(r"\d(product|product_narrow|product_wide|product_wide_e4m3|gate|quant_mx4|dequant_mx4)_kernelI")
+NEW = re.compile(r"\d(product|product_narrow|product_wide|gate|quant_mx4|dequant_mx4)_kernelI")
 WIDE = re.compile(r"product_wide_kernelI")           # spills at the ends of tiles, some bytes more or less
 LOOSE = re.compile(r"product_kernelI.*Lb0ELi[12]E")  # operands off the grid, in registers
 
@@ -13,7 +13,7 @@ LOOSE = re.compile(r"product_kernelI.*Lb0ELi[12]E")  # operands off the grid, in
 def test_scratch(kernels):  # noqa: F811
     got = {n: scratch for n, (_, scratch) in kernels.items() if NEW.search(n)}
     assert len([n for n in got if "product_narrow" in n]) == 16
-    assert len([n for n in got if "product_wide_e4m3" in n]) == 3
+    assert len([n for n in got if "product_wide_kernelINS_5PE4M3" in n]) == 3
     assert len([n for n in got if "gate_kernel" in n]) == 6 and len([n for n in got if "mx4_kernel" in n]) == 6
     most = lambda n: 800 if WIDE.search(n) else 128 if LOOSE.search(n) else 0
     bad = [(n, s) for n, s in got.items() if s > most(n)]
