@@ -1,6 +1,7 @@
 // xred_layer.hip -- the C ABI of the calls around a reduced activation:
 // argument checks and dispatch to the launchers (xred_norm.hip, xred_route.hip,
-// xred_experts.hip, xred_product_*.hip, xred_gate.hip, xred_mx4.hip).  As elsewhere, everything is checked before anything is enqueued.
+// xred_experts.hip, xred_product.hip, xred_gate.hip, xred_mx4.hip).  As elsewhere,
+// everything is checked before anything is enqueued.
 #include "xred_layer.hpp"
 
 #define TRY(call)                                    \
@@ -108,8 +109,7 @@ xred_status check_slots(uint64_t tokens, uint32_t topk, uint64_t hidden, uint64_
     return XRED_SUCCESS;
 }
 
-// What the experts' products share: sizes.  `tiles`: the most that a launch has, of the
-// smallest kind.
+// What the experts' products share: sizes.  `tiles`: no launch has more of any kind.
 xred_status check_product(uint64_t rows, uint64_t n, uint64_t k, uint32_t experts, bool grad)
 {
     if (experts < 1 || experts > XRED_MAX_EXPERTS)

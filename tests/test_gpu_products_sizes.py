@@ -254,3 +254,42 @@ def test_rows_past_4_gib(xr):
         xr.group_product_grad(out, x, offsets, dw)
         a, b = out[rows - 1000:rows - 10].double(), x[rows - 1000:rows - 10].double()
         check_sum(dw[1], a.t() @ b, a.abs().t() @ b.abs(), 990)
+
+
+@pytest.mark.parametrize("far", ["x", "w", "out", "scale"])
+def test_rows_far_apart(xr, far):
+    """8 MB and more from row to row: few rows, many, and a gradient."""
+    g = generator(14)
+    apart = (1 << 23) + 16
+
+    def spaced(t, yes):
+        if not yes:
+            return t
+        rows, n = t.shape
+        store = torch.empty(rows * apart, dtype=t.dtype, device="cuda")
+        view = store.view(rows, apart)[:, :n]
+        view.copy_(t)
+        return view
+
+    for counts, n, k in (([3, 2], 72, 136), ([30, 35], 72, 136), ([1, 0, 2], 130, 264)):
+        rows, experts, offsets = sum(counts), len(counts), offsets_of(counts)
+        x, w = normal(g, rows, k).bfloat16(), normal(g, experts * n, k).bfloat16()
+        out = spaced(torch.full((rows, n), SENTINEL, dtype=torch.bfloat16, device="cuda"), far == "out")
+        w_far = spaced(w, far == "w").unflatten(0, (experts, n)) if experts * n <= 150 else w.view(experts, n, k)
+        x_far = spaced(x, far == "x")
+        xr.group_product(x_far, w_far, offsets, out)
+        check_sum(out, *product(x, w.view(experts, n, k), offsets), k, (far, n))
+        dw = torch.empty(experts, n, k, device="cuda")
+        d = normal(g, rows, n).bfloat16()
+        xr.group_product_grad(spaced(d, far == "out"), x_far, offsets, dw)
+        at = offsets.tolist()
+        for e in range(experts):
+            a, b = d[at[e]:at[e + 1]].double(), x[at[e]:at[e + 1]].double()
+            check_sum(dw[e], a.t() @ b, a.abs().t() @ b.abs(), counts[e] + 1)
+        x4, scale = quant_mx4(x.float())
+        w4, w_scale = quant_mx4(w.float())
+        w4, w_scale = w4.view(experts, n, -1), w_scale.view(experts, n, -1)
+        out = torch.full((rows, n), SENTINEL, dtype=torch.bfloat16, device="cuda")
+        xr.group_product(spaced(x4, far == "x"), w4, offsets, out, scale=spaced(scale, far == "scale"),
+                         w_scale=w_scale)
+        check_sum(out, *product(of_mx4(x4, scale), of_mx4(w4, w_scale), offsets), k, (far, n))
