@@ -670,7 +670,8 @@ enum { XRED_PRODUCT_ADD = 1u };                                /* xred_group_pro
  * the weights being n x k for each expert, or k x n with XRED_PRODUCT_TRANSPOSE
  * (w[e][j][i]: the gradient of the rows takes the forward call's weights so).
  * Other rows of out are left untouched.  Sums are binary32, in an order that depends
- * on the sizes alone.
+ * on the types and sizes (rows, n, k, experts) alone, not on where the operands lie, how
+ * far apart their rows are, or how much of the chip the device is.
  *   dtype    XRED_FLOAT32, XRED_BFLOAT16, XRED_FLOAT16: x and w, no scales.
  *            XRED_FP8_E4M3: up(x[r][j]) is x * scale[r][j / 128], up(w[e][i][j]) is
  *            w * w_scale[e][i / 128][j / 128], all scales binary32; each 128

@@ -447,9 +447,13 @@ __device__ __forceinline__ float value_at(const char *row, uint32_t c, xred_dtyp
 // TFLOP/s; the gradient of 515 x 1027 fp32, 8 experts, 1800 rows 40 us, 18 of them matrix
 // instructions).
 // Two of the larger tiles or four of the smaller have to fit a CU: while one waits for its
-// loads, another multiplies (one: 4200 us where two take 2210).
-template <class P, bool GRAD, bool ACROSS, bool DIRECT, int RB, int CB>
-__global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kernel(ProductParams p)
+// loads, another multiplies (one: 4200 us where two take 2210; with HALVES, rare, two).
+//
+// HALVES: each half of the steps, sub-steps 0 and 1 and sub-steps 2 and 3, has sums of its own,
+// which meet at the end, as in the streaming tiles (xred_product_narrow.hpp), in whose place
+// these take rows 8 MB and more apart: the same bits at any distance.
+template <class P, bool GRAD, bool ACROSS, bool DIRECT, int RB, int CB, bool HALVES>
+__global__ __launch_bounds__(kProductThreads, RB == 2 || HALVES ? 2 : 4) void product_kernel(ProductParams p)
 {
     constexpr int BM = 64 * RB, BN = 64 * CB;
     using Rows = std::conditional_t<DIRECT, GridOperand<P, GRAD, BM>, LooseOperand<P, GRAD, BM, uint64_t>>;
@@ -511,11 +515,11 @@ __global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kern
         const uint32_t col_length = ACROSS && !GRAD ? p.k : length;
         rows.start(from, p.row_stride, items, length);
         columns.start(col_from, p.col_stride, p.n - n0, col_length);
-        f32x16 acc[RB][CB];
+        f32x16 acc[RB][CB], late[RB][CB];   // HALVES: of the second half in late
 #pragma unroll
         for (int r = 0; r < RB; ++r)
 #pragma unroll
-            for (int c = 0; c < CB; ++c) acc[r][c] = f32x16{};
+            for (int c = 0; c < CB; ++c) acc[r][c] = late[r][c] = f32x16{};
 
         const uint32_t per = GRAD ? Rows::kRows : 128;
         const uint32_t steps = (length + per - 1) / per;
@@ -553,10 +557,16 @@ __global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kern
                     for (int c = 0; c < CB; ++c) {
                         const float by = a * *(const float *)(cs[c] + t * 4ull);
                         f32x16 part = multiply_e4m3(cf[0][c], cf[1][c], rf[0][r], rf[1][r], f32x16{});
-                        part = multiply_e4m3(cf[2][c], cf[3][c], rf[2][r], rf[3][r], part);
+                        if constexpr (HALVES) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            acc[r][c][j] = __builtin_fmaf(part[j], by, acc[r][c][j]);
+                            for (int j = 0; j < 16; ++j)
+                                acc[r][c][j] = __builtin_fmaf(part[j], by, acc[r][c][j]);
+                            part = f32x16{};
+                        }
+                        part = multiply_e4m3(cf[2][c], cf[3][c], rf[2][r], rf[3][r], part);
+                        f32x16 &to = HALVES ? late[r][c] : acc[r][c];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) to[j] = __builtin_fmaf(part[j], by, to[j]);
                     }
                 }
             } else {
@@ -588,10 +598,11 @@ __global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kern
                     for (int r = 0; r < RB; ++r)
 #pragma unroll
                         for (int c = 0; c < CB; ++c) {
+                            f32x16 &to = HALVES && S >= 2 ? late[r][c] : acc[r][c];
                             if constexpr (__is_same(P, PMx4))
-                                acc[r][c] = multiply_mx4<S>(cf[c], rf[r], ce[c], re[r], acc[r][c]);
+                                to = multiply_mx4<S>(cf[c], rf[r], ce[c], re[r], to);
                             else
-                                acc[r][c] = multiply<P>(cf[c], rf[r], acc[r][c]);
+                                to = multiply<P>(cf[c], rf[r], to);
                         }
                 };
                 sub_step(std::integral_constant<int, 0>{});
@@ -628,6 +639,11 @@ __global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kern
                 if (t + 1 < steps) step(t + 1, r0, c0, r1, c1);
             }
         }
+        if constexpr (HALVES)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int c = 0; c < CB; ++c) acc[r][c] += late[r][c];
         char *out = p.out + (GRAD ? e * p.out_expert : 0) + m0 * p.out_stride;
         auto leave = [&](uint32_t row, uint32_t col, float (&v)[4]) {
             if (row >= items || col >= p.n) return;
@@ -682,7 +698,7 @@ __global__ __launch_bounds__(kProductThreads, RB == 2 ? 2 : 4) void product_kern
     }
 }
 
-template <class P, bool GRAD, bool ACROSS, bool DIRECT, int RB, int CB>
+template <class P, bool GRAD, bool ACROSS, bool DIRECT, int RB, int CB, bool HALVES = false>
 hipError_t go_product(ProductParams p, hipStream_t s)
 {
     constexpr uint32_t BM = 64 * RB, BN = 64 * CB;
@@ -691,7 +707,7 @@ hipError_t go_product(ProductParams p, hipStream_t s)
     // forward: every expert may end in a tile that is not whole
     const uint64_t tiles = GRAD ? (uint64_t)p.experts * p.row_tiles
                                 : p.rows / BM + (p.rows < p.experts ? p.rows : p.experts);
-    return launch_kernel(product_kernel<P, GRAD, ACROSS, DIRECT, RB, CB>,
+    return launch_kernel(product_kernel<P, GRAD, ACROSS, DIRECT, RB, CB, HALVES>,
                          dim3(grid_of((tiles * p.col_tiles + 7) / 8 * 8, kProductThreads)),
                          dim3(kProductThreads), 0, s, p);
 }

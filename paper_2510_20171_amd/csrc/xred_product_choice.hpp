@@ -1,4 +1,8 @@
 // xred_product_choice.hpp -- which kernel takes a product, by types, sizes and alignment.
+//
+// Results have the same bits whatever the alignment, the distance between rows and the part
+// of the chip that the device is: all kernels add in the same order, but for the streaming
+// ones, which sum each half of the steps by itself, and those are chosen by types and sizes alone.
 #pragma once
 
 #include "xred_product_narrow.hpp"
@@ -27,13 +31,22 @@ inline bool wide_pays(const ProductParams &p, bool grad, bool f32)
 // 64 experts, 2048 rows of 299 x 2045 23 and 38; from 64 x 64 tiles for every CU on it turns:
 // 8 experts, 2000 rows of 640 x 320 7.8 and 6.2).  At 64 elements and more, which pieces and
 // mx4's exponents are read in whole.
+constexpr uint64_t kChipCus = 256;   // of the whole chip, even if the device is a part of it
 inline bool narrow_pays(const ProductParams &p)
 {
     if (p.n < 64 || p.k < 64) return false;
     const uint64_t tiles = (p.rows / 64 + (p.rows < p.experts ? p.rows : p.experts)) * (uint64_t)((p.n + 63) / 64);
-    const uint64_t cus = device_cus();
-    return (p.rows <= 16ull * p.experts || tiles <= cus || (p.rows <= 32ull * p.experts && tiles < 2 * cus)) &&
-           p.row_stride < kWideStride && p.col_stride < kWideStride;
+    return p.rows <= 16ull * p.experts || tiles <= kChipCus ||
+           (p.rows <= 32ull * p.experts && tiles < 2 * kChipCus);
+}
+
+// Rows 8 MB and more apart are past the streaming tiles' 32-bit offsets.
+template <class P, bool ACROSS, bool DIRECT>
+hipError_t go_few(const ProductParams &p, hipStream_t s)
+{
+    return p.row_stride < kWideStride && p.col_stride < kWideStride
+               ? go_narrow<P, ACROSS, DIRECT>(p, s)
+               : go_product<P, false, ACROSS, DIRECT, 1, 1, true>(p, s);
 }
 
 // Tiles of 64 x 64 where there are too few of 128 x 128 to keep the chip busy, and in fp32,
@@ -60,8 +73,8 @@ hipError_t launch_product_plain(const ProductParams &p, bool grad, bool across, 
                                    on_grid(p.col, p.col_stride, p.col_expert, (across ? p.n : p.k) * es);
     if (!grad && narrow_pays(p)) {
         if (across)
-            return direct ? go_narrow<P, true, true>(p, s) : go_narrow<P, true, false>(p, s);
-        return direct ? go_narrow<P, false, true>(p, s) : go_narrow<P, false, false>(p, s);
+            return direct ? go_few<P, true, true>(p, s) : go_few<P, true, false>(p, s);
+        return direct ? go_few<P, false, true>(p, s) : go_few<P, false, false>(p, s);
     }
     if (p.row_stride < kWideStride && p.col_stride < kWideStride && wide_pays(p, grad, es == 4)) {
         using O = typename OwnType<P>::T;
@@ -98,7 +111,7 @@ hipError_t launch_product_scaled(const ProductParams &p, hipStream_t s)
     const bool direct = on_grid(p.row, p.row_stride, 0, p.k) &&
                         on_grid(p.col, p.col_stride, p.col_expert, p.k);
     if (narrow_pays(p))
-        return direct ? go_narrow<P, false, true>(p, s) : go_narrow<P, false, false>(p, s);
+        return direct ? go_few<P, false, true>(p, s) : go_few<P, false, false>(p, s);
     if (direct && p.row_stride < kWideStride && p.col_stride < kWideStride && scale_words<P>(p) &&
         wide_pays(p, false, false))
         return p.out_type == XRED_FLOAT32    ? launch_wide<P, TF32>(p, false, false, s)
