@@ -687,7 +687,8 @@ enum { XRED_PRODUCT_ADD = 1u };                                /* xred_group_pro
  *            dtype itself or XRED_FLOAT32
  *   rows     of x and out, below 2^31; n, k: 1..XRED_MAX_PRODUCT
  *   offsets  experts + 1 int32 in device memory, ascending; what lies outside
- *            [0, rows] is cut off.  experts: 1..XRED_MAX_EXPERTS
+ *            [0, rows] is cut off.  Out of order, they make some rows of out hold
+ *            anything, but no more work than rows allows.  experts: 1..XRED_MAX_EXPERTS
  *   w        expert 0's weights; the others follow w_expert elements apart each
  *            (mx4: bytes, as are the distances of x, w and their scales).
  *   scale    rows x ceil(k / 128) (mx4: ceil(k / 32) bytes); w_scale: ceil(n / 128) x

@@ -371,10 +371,12 @@ struct RowTiles {
         }
 #pragma unroll
         for (int j = 0; j < kEach; ++j) first[j] += before;
+        // offsets out of order: a workgroup's places must not wrap round on the way there
+        total = total < p.most ? total : p.most;
     }
 
     // Tile t (below total): its expert and rows [lo, hi), into found[3] (LDS).  Offsets that do
-    // not ascend can make total overflow, and then none is found.
+    // not ascend can make the sum overflow, and then none is found.
     __device__ __forceinline__ void find(uint32_t t, uint32_t rows_of_tile, uint32_t *found) const
     {
         __syncthreads();   // the tile before has been read
@@ -707,6 +709,7 @@ hipError_t go_product(ProductParams p, hipStream_t s)
     // forward: every expert may end in a tile that is not whole
     const uint64_t tiles = GRAD ? (uint64_t)p.experts * p.row_tiles
                                 : p.rows / BM + (p.rows < p.experts ? p.rows : p.experts);
+    p.most = (uint32_t)tiles;
     return launch_kernel(product_kernel<P, GRAD, ACROSS, DIRECT, RB, CB, HALVES>,
                          dim3(grid_of((tiles * p.col_tiles + 7) / 8 * 8, kProductThreads)),
                          dim3(kProductThreads), 0, s, p);

@@ -21,6 +21,7 @@ struct ProductParams {
     uint32_t k;         // forward: elements summed over (mx4: bytes, two elements each)
     uint32_t experts;
     uint32_t row_tiles, col_tiles;   // set by the launcher
+    uint32_t most;                   // the same: what RowTiles counts, at most, of offsets that ascend
     uint32_t spans;                  // the same: several columns of an expert's last rows in one
     xred_dtype out_type;
     uint32_t add;

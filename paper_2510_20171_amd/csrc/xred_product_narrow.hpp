@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kProductThreads, 3) void product_narrow_kernel(Prod
             i -= __builtin_amdgcn_readfirstlane(first[w.expert]);
             uniform_rows(p, w.expert, lo, hi);
             tiles = (hi - lo + BM - 1) / BM;   // side by side: the same weights
-            // else offsets do not ascend, and total has overflowed
+            // else offsets do not ascend, and the sum has overflowed
             if (i < tiles * p.col_tiles) break;
         }
         place += gridDim.x;
@@ -234,6 +234,7 @@ hipError_t go_narrow(ProductParams p, hipStream_t s)
 {
     p.col_tiles = (p.n + 63) / 64;
     const uint64_t tiles = (p.rows / 32 + (p.rows < p.experts ? p.rows : p.experts)) * (uint64_t)p.col_tiles;
+    p.most = (uint32_t)tiles;
     const uint64_t most = 3 * device_cus();   // at once
     return launch_kernel(product_narrow_kernel<P, ACROSS, GRID>,
                          dim3(grid_of(tiles < most ? (tiles + 7) / 8 * 8 : most, kProductThreads)),

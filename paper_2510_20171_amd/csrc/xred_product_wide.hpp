@@ -264,7 +264,7 @@ __device__ __forceinline__ void product_wide(const ProductParams &p)
                 w.expert = __builtin_amdgcn_readfirstlane(upto - 1);
                 i -= __builtin_amdgcn_readfirstlane(first[w.expert]);
                 uniform_rows(p, w.expert, lo, hi);
-                // else offsets do not ascend, and total has overflowed
+                // else offsets do not ascend, and the sum has overflowed
                 if (i < items_of(hi - lo)) break;
             }
             place += gridDim.x;
@@ -748,6 +748,7 @@ hipError_t go_wide(ProductParams p, hipStream_t s)
     p.row_tiles = (p.m + 255) / 256;
     const uint64_t tiles = (GRAD ? (uint64_t)p.experts * p.row_tiles
                                  : p.rows / 256 + (p.rows < p.experts ? p.rows : p.experts)) * p.col_tiles;
+    p.most = (uint32_t)tiles;
     // a workgroup on every CU, which takes what there is in turns
     const uint64_t cus = device_cus();
     // even out what workgroups do where each has enough items (12 a CU: 678 us without, 653
