@@ -734,7 +734,11 @@ XRED_API xred_status xred_group_product_grad(const xred_group_product_grad_args 
  *     y = g * s * u,   s = 1 / (1 + exp(-g)),   g = up(x[r][i]), u = up(x[r][width + i])
  *     out = down(y),   out8 = e4m3(y / scale),  scale as xred_fold_norm's
  * for the rows below *count (an int32 in device memory, such as offsets[experts]), or
- * for all of them where count is NULL; the others are left untouched.
+ * for all of them where count is NULL; the others are left untouched.  y is not rounded
+ * before it is scaled; scale and y / scale are as good as xred_fold_norm's, so a quotient
+ * that close to the middle of two e4m3 values may become either.  Infinite gates and values
+ * give what binary32 gives (a gate of -infinity: 0 times infinity, NaN); an infinite y gives
+ * an infinite scale, its own code NaN and the group's others 0.
  *   out, out8   rows x width, each optional, at least one present
  *   scale       rows x ceil(width / group) binary32, present with out8
  *   group       32, 64, 128, 256 or 512, with out8
