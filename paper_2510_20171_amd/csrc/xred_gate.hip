@@ -2,7 +2,7 @@
 // its gradient (xred_gate_grad).
 //
 // Bound by HBM: two elements in and one out (8-bit: with a scale for each group), three
-// in and two out for the gradient (29500 x 2048 bf16 to e4m3 69 us, 4.4 TB/s; gradient of
+// in and two out for the gradient (29500 x 2048 bf16 to e4m3 69 to 76 us, 4.4 TB/s; gradient of
 // 7370 x 2501 34 us, 5.4 TB/s).  Each lane has 8 gates and their 8 values at once,
 // so a group's largest is a maximum over 4 to 64 neighbouring lanes.
 #include "xred_sigmoid.hpp"

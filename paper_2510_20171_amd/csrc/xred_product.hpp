@@ -444,7 +444,8 @@ __device__ __forceinline__ float value_at(const char *row, uint32_t c, xred_dtyp
 // ------------------------------------------------------------------ kernel --
 // 4 waves, two by two, each RB x CB blocks of 32 x 32: tiles of 64 RB x 64 CB, one step of
 // k multiplied while the next is on its way.  What the wider and the narrower tiles do not
-// take: few tiles, short rows, strides of 8 MB and more, gradients off the 16-byte grid.
+// take: n or k below 64, rows 8 MB and more apart, fp32 but for thousands of tiles, gradients of
+// few tiles or off the 16-byte grid, forward products with fewer tiles than the wider ones need.
 // Bound by that way from memory (32768 rows, 4096 x 2048 bf16 would take 1340 us, 410
 // TFLOP/s; the gradient of 515 x 1027 fp32, 8 experts, 1800 rows 40 us, 18 of them matrix
 // instructions).

@@ -31,6 +31,11 @@ inline bool wide_pays(const ProductParams &p, bool grad, bool f32)
 // 64 experts, 2048 rows of 299 x 2045 23 and 38; from 64 x 64 tiles for every CU on it turns:
 // 8 experts, 2000 rows of 640 x 320 7.8 and 6.2).  At 64 elements and more, which pieces and
 // mx4's exponents are read in whole.
+//
+// The host knows the rows that x has, not those that exist or which expert has them.  64 experts
+// of 4096 x 2048 bf16, in a buffer of 32768 rows (wide tiles) and in one of their own size: 4096
+// rows 250 and 203 us, 512 rows 232 and 181, 64 rows 119 and 110.  256 experts of 2048 x 2048,
+// 4096 rows, narrow tiles: 374 us with 16 rows each, 425 with 3841 of them in one expert.
 constexpr uint64_t kChipCus = 256;   // of the whole chip, even if the device is a part of it
 inline bool narrow_pays(const ProductParams &p)
 {

@@ -1,15 +1,16 @@
-// xred_product_narrow.hpp -- the experts' products of few rows each: a decode batch.
+// xred_product_narrow.hpp -- the experts' products of few rows each, a decode batch, and of
+// too few tiles to fill the chip with larger ones.
 //
-// Bound by HBM: every used expert's weights are read once, and all that counts is to keep
-// enough of them on their way.  A tile is 32 rows by 64 columns; four steps of k lie in
-// LDS (48 KB, so that three workgroups share a CU), three of them on their way at any
-// time, and go on from a tile into the next one without a pause.  Two waves have a block
-// of 32 columns each for one half of every step, two for the other half; the halves meet in
-// LDS at the tile's end.
+// Bound by HBM: the weights of every expert that has rows are read once (from L2 again for
+// every 32 rows more), and all that counts is to keep enough of them on their way.  A tile is
+// 32 rows by 64 columns; four steps of k lie in LDS (48 KB, so that three workgroups share a
+// CU), three of them on their way at any time, and go on from a tile into the next one without
+// a pause.  Two waves have a block of 32 columns each for one half of every step, two for the
+// other half; the halves meet in LDS at the tile's end.
 //
-// 8 rows of 64 experts, 4096 x 4096: bf16 47 us, 5.7 TB/s (128 x 128 tiles, one step on its
-// way: 71), transposed 61 (100), e4m3 26 (33), mx4 17 (31), 4097 x 4099 bf16 88 (116).  488
-// rows of 128 experts, mx4: 168 us, 6.8 TB/s (280).
+// 8 rows of 64 experts, 4096 x 4096: bf16 50 us, 5.4 TB/s (128 x 128 tiles, one step on its
+// way: 71), transposed 65 (100), e4m3 32 (33), mx4 17 (31), 4097 x 4099 bf16 98 (116).  488
+// rows of 128 experts, of which 86 have some, mx4: 168 us, 4.7 TB/s (280).
 #pragma once
 
 #include "xred_product_wide.hpp"

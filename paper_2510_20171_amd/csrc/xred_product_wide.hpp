@@ -2,7 +2,7 @@
 // enough rows to fill the chip with them.
 //
 // Bound by the matrix cores (32768 rows of 64 experts, 4096 x 2048 bf16: 0.55 TFLOP, 390 us at
-// a large library product's rate, 613 here; one expert 1217 TFLOP/s; 128 x 128 tiles 1340 us).
+// a large library product's rate, 621 to 645 here; one expert 1217 TFLOP/s; 128 x 128 tiles 1340 us).
 //
 // A workgroup of four waves has a CU to itself: each wave keeps 128 x 128 sums in its
 // 256 accumulation registers, so that a fragment of either operand is used four times
@@ -18,12 +18,12 @@
 // has a main loop of its own that does a half or a quarter of the products.
 //
 // mx4: exponents of two steps at a time lie in LDS beside the operands, each lane's own
-// dword of four (32768 rows, 4096 x 4096: 430 us, 2.6 PFLOP/s; 128 x 128 tiles 1100).
+// dword of four (32768 rows, 4096 x 4096: 430 to 470 us, 2.3 to 2.6 PFLOP/s; 128 x 128 tiles 1100).
 //
 // e4m3: a step is the 128 elements that share their scales.  Its sums are scaled by vector
 // instructions, 16 for two matrix instructions, and join sums of binary32: a tile of 256 x
 // 128 leaves registers for them, and three steps in LDS since each is half the work for as
-// long a way from memory (29500 rows, 4096 x 4096: 843 us, 1.17 PFLOP/s; two steps and 256
+// long a way from memory (29500 rows, 4096 x 4096: 853 us, 1.16 PFLOP/s; two steps and 256
 // x 128 1070, 128 x 128 tiles 1196).
 //
 // Workgroups stay for several tiles.  The first two steps of the next tile are loaded
